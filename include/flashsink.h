@@ -378,6 +378,104 @@ fs_status fs_points_keep(fs_ctx *ctx, const fs_problem *prob);
 fs_status fs_points_release(fs_ctx *ctx);
 
 /*
+ * Operators of a network that is trained on this library's losses.  They share the conventions above (device pointers
+ * owned by the caller, work enqueued on the context's stream, status codes) and use the context's second buffer for
+ * partial results, so copies that fs_points_keep declares stay.  None of them synchronises, but for a call that has to grow
+ * that buffer.  Nothing is added by atomics: results do not depend on the order in which workgroups run.
+ */
+
+/*
+ * Softmax attention of many sets and heads, the form of Prop. 3 with separate queries, keys and values:
+ *   s_ij = scale <q_i, k_j> + bias_j,   o_i = sum_j exp(s_ij - m_i) v_j / l_i,   m_i = max_j s_ij,  l_i = sum_j exp(s_ij - m_i)
+ * over the keys j that row i of a set sees: j < k_len, and with `causal` also j <= i + k_len - q_len (the last query sees the
+ * last key).  Rows i >= q_len, and rows that see no key or only keys with bias -inf, have o_i = 0, m_i = -inf, l_i = 0
+ * and pass no gradient on.  Keys that are not seen by any row (j >= k_len, or bias -inf) are not read into the result whatever
+ * they hold, NaN included, and their gradients are 0.  A bias of the type's lowest value is a number like any other.
+ * kv_heads divides q_heads; head h reads keys and values of head h / (q_heads / kv_heads).  d <= 128 coordinates.
+ * Lengths may be 0 and 1, strides are in elements, any alignment will do (rows of whole 16 bytes, aligned to them, are
+ * read fastest).
+ * FS_F32: products on the fp32 matrix cores.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
+ * probabilities (2^-9 of each) and their gradients are rounded to bf16 where they enter a second product.  Maxima, sums
+ * and accumulators are fp32 in both.
+ */
+typedef struct {
+    void *data;               /* element (set 0, row 0, head 0, coordinate 0); coordinates are contiguous */
+    int64_t batch, row, head; /* strides in elements, >= 0                                                */
+} fs_heads;
+
+typedef struct {
+    fs_heads q, k, v;                 /* q: batch x q_rows x q_heads x d; k, v: batch x k_rows x kv_heads x d     */
+    int32_t dtype;                    /* fs_dtype of q, k, v, of the output, and of all gradients                 */
+    int32_t causal;                   /* 0 or 1                                                                   */
+    int64_t batch, q_rows, k_rows;    /* each may be 0; rows <= 2^24                                              */
+    int64_t q_heads, kv_heads, d;
+    float scale;                      /* positive and finite                                                      */
+    const int32_t *q_len, *k_len;     /* [batch], device, or NULL: all rows; taken into 0 .. q_rows (k_rows)      */
+    const float *bias;                /* [batch][k_rows], device, or NULL                                         */
+    int64_t bias_ld;                  /* elements from one set's bias to the next, >= k_rows or 0 (shared)        */
+} fs_attn;
+
+/* o: written, q's shape (strides >= d); stat: [batch][q_heads][q_rows][2] floats, aligned to 8 bytes, receives (m_i, l_i). */
+fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, float *stat /* device */);
+
+/*
+ * Gradients of fs_attention for the gradient d_o of its output: dq, dk, dv (q's, k's and v's shapes, all written; summed
+ * over the heads that share keys), and dbias [batch][k_rows] of `dtype` (stride dbias_ld >= k_rows), NULL to skip.  o and
+ * stat are what fs_attention gave.  The probabilities are computed anew from stat; no n x m matrix is stored.
+ */
+fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, const float *stat /* device */, const fs_heads *d_o,
+                            const fs_heads *dq, const fs_heads *dk, const fs_heads *dv, void *dbias /* device, nullable */,
+                            int64_t dbias_ld);
+
+/*
+ * Layer norm over the columns of x (rows x cols, ldx):  y = (x - mean) rstd gamma + beta,  rstd = 1 / sqrt(var + eps),
+ * var the mean squared deviation.  gamma, beta: cols values of `wtype`, or NULL (1, 0).  stat: NULL or rows x 2 floats,
+ * aligned to 8 bytes, receiving (mean, rstd).  x and y of `dtype`; computed in fp32.  rows may be 0.  eps >= 0.
+ */
+fs_status fs_layer_norm(fs_ctx *ctx, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma,
+                        const void *beta, int32_t wtype, float eps, void *y, int64_t ldy, float *stat /* device, nullable */);
+
+/*
+ * Its gradients, from the stat of the forward pass:  dx (NULL to skip), dgamma = sum over rows of dy xh and dbeta = sum of dy
+ * (cols floats each, NULL to skip).  dx of `dtype`; dx may be dy itself (same address and stride).
+ */
+fs_status fs_layer_norm_grad(fs_ctx *ctx, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma,
+                             int32_t wtype, const float *stat, const void *dy, int64_t lddy, void *dx, int64_t lddx, float *dgamma,
+                             float *dbeta);
+
+/*
+ * One AdamW step over `count` tensors (decoupled weight decay):
+ *   g' = g * grad_scale,   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
+ *   p = (1 - lr weight_decay) p - (lr / (1 - beta1^step)) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * computed in fp32.  state_bits 32: m and v are floats.  state_bits 8: m and v are OCP e4m3 codes (one byte each) of m and of
+ * sqrt(v), under one power of two for every 256 consecutive weights (m_scale, v_scale: ceil(n / 256) floats; value = code *
+ * scale; a fresh state is codes of 0 and scales of 1).  Codes are rounded up or down in proportion by bits that are a function
+ * of `seed` and of the weight's number in the call: the same call gives the same codes, another seed another rounding.
+ * A block with a value that is not finite gets scales of NaN.
+ * bf16 weights may have float masters: these are then updated, and p receives them rounded.  Tensors are contiguous, of any
+ * alignment (16 bytes is fastest), n may be 0; no two of them may overlap.
+ */
+typedef struct {
+    void *p;                    /* n weights of p_dtype, in/out                               */
+    const void *g;              /* n gradients of g_dtype                                     */
+    float *master;              /* n floats, in/out, or NULL; for all tensors or for none     */
+    void *m, *v;                /* n floats or n codes each, in/out                           */
+    float *m_scale, *v_scale;   /* state_bits 8: in/out; otherwise not looked at              */
+    int64_t n;
+} fs_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay >= 0; betas in [0, 1) */
+    int64_t step;                                 /* 1 for the first step                        */
+    int32_t p_dtype, g_dtype;                     /* fs_dtype                                    */
+    int32_t state_bits;                           /* 32 or 8                                     */
+    uint32_t seed;
+    const float *grad_scale;                      /* device scalar, or NULL: 1                   */
+} fs_adamw_args;
+
+fs_status fs_adamw(fs_ctx *ctx, const fs_adamw_args *args /* host */, const fs_adamw_tensor *tensors /* host */, int32_t count);
+
+/*
  * Test and experiment switches of ONE context (there is no process-wide state; a new context has
  * every switch at 0 = the library decides).  Not needed for normal use.
  *   "lowd_splits"        1..1024: split count of the streamed side of the d <= 16 passes

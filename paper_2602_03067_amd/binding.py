@@ -22,7 +22,7 @@ FS_COMPUTE_FP32, FS_COMPUTE_BF16_MFMA = 0, 1
 EXPORTS = (
     "fs_create", "fs_destroy", "fs_status_str", "fs_last_error", "fs_version", "fs_row_norms",
     "fs_update_f", "fs_update_g", "fs_solve", "fs_solve_noalloc", "fs_solve_labeled", "fs_solve_symmetric", "fs_solve_tol", "fs_marginal_err", "fs_ot_value", "fs_check_weights", "fs_check_finite", "fs_divergence", "fs_apply_plan",
-    "fs_apply_plan_T", "fs_apply_plan_hadamard", "fs_grad_x", "fs_grad_y", "fs_hvp", "fs_points_keep", "fs_points_release", "fs_debug_set", "fs_debug_get", "fs_profile_enable", "fs_profile_read",
+    "fs_apply_plan_T", "fs_apply_plan_hadamard", "fs_grad_x", "fs_grad_y", "fs_hvp", "fs_attention", "fs_attention_grad", "fs_layer_norm", "fs_layer_norm_grad", "fs_adamw", "fs_points_keep", "fs_points_release", "fs_debug_set", "fs_debug_get", "fs_profile_enable", "fs_profile_read",
 )
 
 
@@ -34,6 +34,30 @@ class FsProblem(ctypes.Structure):
         ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64),
         ("a", ctypes.c_void_p), ("b", ctypes.c_void_p),
     ]
+
+
+class FsHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class FsAttn(ctypes.Structure):
+    _fields_ = [
+        ("q", FsHeads), ("k", FsHeads), ("v", FsHeads), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+        ("batch", ctypes.c_int64), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
+        ("q_heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("d", ctypes.c_int64), ("scale", ctypes.c_float),
+        ("q_len", ctypes.c_void_p), ("k_len", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("bias_ld", ctypes.c_int64),
+    ]
+
+
+class FsAdamwTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class FsAdamwArgs(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("p_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32), ("seed", ctypes.c_uint32), ("grad_scale", ctypes.c_void_p)]
 
 
 class FlashSinkError(RuntimeError):
@@ -85,6 +109,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fs_grad_x.argtypes = [vp, PP, f32, vp, vp, i32, vp, i64]
     lib.fs_grad_y.argtypes = [vp, PP, f32, vp, vp, i32, vp, i64]
     lib.fs_hvp.argtypes = [vp, PP, f32, vp, vp, vp, i64, f32, f32, i32, vp, i64, ctypes.POINTER(i32)]
+    PH = ctypes.POINTER(FsHeads)
+    lib.fs_attention.argtypes = [vp, ctypes.POINTER(FsAttn), PH, vp]
+    lib.fs_attention_grad.argtypes = [vp, ctypes.POINTER(FsAttn), PH, vp, PH, PH, PH, PH, vp, i64]
+    lib.fs_layer_norm.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i32, f32, vp, i64, vp]
+    lib.fs_layer_norm_grad.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, vp, vp, i64, vp, i64, vp, vp]
+    lib.fs_adamw.argtypes = [vp, ctypes.POINTER(FsAdamwArgs), ctypes.POINTER(FsAdamwTensor), i32]
     lib.fs_debug_set.argtypes = [vp, ctypes.c_char_p, i64]
     lib.fs_debug_get.argtypes = [vp, ctypes.c_char_p, ctypes.POINTER(i64)]
     lib.fs_points_keep.argtypes = [vp, PP]
@@ -111,6 +141,60 @@ def _dev_f32(t: torch.Tensor, name: str, shape=None):
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     return t
+
+
+_DTYPES = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
+
+
+def _heads(t: torch.Tensor, name: str, shape, dtype) -> FsHeads:
+    """The C view of a (sets, rows, heads, coordinates) tensor."""
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError("%s must be a %s tensor on the GPU" % (name, dtype))
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    b, r, h, e = t.stride()
+    if e != 1 and shape[3] != 1:
+        raise ValueError("%s must have unit stride within a head" % name)
+    return FsHeads(t.data_ptr(), b, r, h)
+
+
+def _lengths(t: Optional[torch.Tensor], name: str, batch: int):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.shape != (batch,):
+        raise TypeError("%s must be a contiguous int32 GPU tensor of %d lengths" % (name, batch))
+    return t.data_ptr()
+
+
+def _attn(q, k, v, scale, causal, q_len, k_len, bias) -> FsAttn:
+    if q.dim() != 4 or k.dim() != 4 or q.dtype not in _DTYPES:
+        raise TypeError("q, k, v must be float32 or bfloat16 tensors of (sets, rows, heads, coordinates)")
+    (batch, n, heads, d), (_, m, kv_heads, _) = q.shape, k.shape
+    a = FsAttn(_heads(q, "q", q.shape, q.dtype), _heads(k, "k", (batch, m, kv_heads, d), q.dtype),
+               _heads(v, "v", (batch, m, kv_heads, d), q.dtype), _DTYPES[q.dtype], 1 if causal else 0, batch, n, m, heads, kv_heads, d,
+               d ** -0.5 if scale is None else scale, _lengths(q_len, "q_len", batch), _lengths(k_len, "k_len", batch), None, 0)
+    if bias is not None:
+        if not bias.is_cuda or bias.dtype != torch.float32 or bias.shape != (batch, m) or (m > 1 and bias.stride(1) != 1):
+            raise TypeError("bias must be a float32 GPU tensor of (sets, keys) with unit inner stride")
+        a.bias, a.bias_ld = bias.data_ptr(), bias.stride(0) if batch > 1 else m
+    return a
+
+
+def _matrix(t: torch.Tensor, name: str):
+    if not t.is_cuda or t.dim() != 2 or t.dtype not in _DTYPES or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError("%s must be a 2-d float32 or bfloat16 GPU tensor with unit inner stride" % name)
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _weights(t: Optional[torch.Tensor], name: str, cols: int):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype not in _DTYPES or t.shape != (cols,) or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous float32 or bfloat16 GPU tensor of %d values" % (name, cols))
+    return t.data_ptr()
 
 
 class Problem:
@@ -345,6 +429,68 @@ class Context:
                     "fs_hvp")
         return out, it.value
 
+    # ---- operators of a network trained on the losses --------------------------------
+    def fs_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: Optional[float] = None, causal: bool = False,
+                     q_len: Optional[torch.Tensor] = None, k_len: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None):
+        """Softmax attention of q (sets, rows, heads, d) over k, v (sets, keys, kv heads, d); returns (o, stat).
+
+        ``scale`` defaults to d^-1/2, ``bias`` (sets, keys) is added to the scores (log-weights; -inf removes a key), ``q_len``,
+        ``k_len`` are the lengths of padded sets.  ``stat`` is what ``fs_attention_grad`` takes up."""
+        a = _attn(q, k, v, scale, causal, q_len, k_len, bias)
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        stat = torch.empty(a.batch, a.q_heads, a.q_rows, 2, dtype=torch.float32, device=q.device)
+        self._check(self.lib.fs_attention(self.h, ctypes.byref(a), ctypes.byref(_heads(o, "o", q.shape, q.dtype)), stat.data_ptr()),
+                    "fs_attention")
+        return o, stat
+
+    def fs_attention_grad(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, stat: torch.Tensor, do: torch.Tensor,
+                          scale: Optional[float] = None, causal: bool = False, q_len: Optional[torch.Tensor] = None,
+                          k_len: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, want_bias: bool = False):
+        """Gradients of ``fs_attention`` (same mask arguments) for the gradient ``do`` of its output: (dq, dk, dv), with ``want_bias``
+        (dq, dk, dv, dbias)."""
+        a = _attn(q, k, v, scale, causal, q_len, k_len, bias)
+        _dev_f32(stat, "stat", (a.batch, a.q_heads, a.q_rows, 2))
+        if want_bias and bias is None:
+            raise ValueError("want_bias without a bias")
+        g = [torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v)]
+        db = torch.empty(bias.shape, dtype=q.dtype, device=q.device) if want_bias else None
+        h = [ctypes.byref(_heads(t, nm, s, q.dtype)) for t, nm, s in
+             ((o, "o", q.shape), (do, "do", q.shape), (g[0], "dq", q.shape), (g[1], "dk", k.shape), (g[2], "dv", k.shape))]
+        self._check(self.lib.fs_attention_grad(self.h, ctypes.byref(a), h[0], stat.data_ptr(), h[1], h[2], h[3], h[4],
+                                               None if db is None else db.data_ptr(), a.k_rows), "fs_attention_grad")
+        return (*g, db) if want_bias else tuple(g)
+
+    def fs_layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5):
+        """Layer norm over the last dimension of x (rows, cols); returns (y, stat) with stat (rows, 2) = (mean, rstd)."""
+        _matrix(x, "x")
+        rows, cols = x.shape
+        w = [_weights(gamma, "gamma", cols), _weights(beta, "beta", cols)]
+        if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+            raise TypeError("gamma and beta must have one type")
+        wt = _DTYPES[gamma.dtype if gamma is not None else beta.dtype if beta is not None else torch.float32]
+        y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+        stat = torch.empty(rows, 2, dtype=torch.float32, device=x.device)
+        self._check(self.lib.fs_layer_norm(self.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), w[0], w[1], wt, eps, y.data_ptr(), cols,
+                                           stat.data_ptr()), "fs_layer_norm")
+        return y, stat
+
+    def fs_layer_norm_grad(self, x: torch.Tensor, gamma: Optional[torch.Tensor], stat: torch.Tensor, dy: torch.Tensor):
+        """Gradients of ``fs_layer_norm`` for the gradient ``dy`` of its output; returns (dx, dgamma, dbeta), the last two float32."""
+        _matrix(x, "x")
+        _matrix(dy, "dy")
+        rows, cols = x.shape
+        if dy.shape != x.shape or dy.dtype != x.dtype:
+            raise ValueError("dy must have the shape and type of x")
+        _dev_f32(stat, "stat", (rows, 2))
+        g = _weights(gamma, "gamma", cols)
+        dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+        dw = torch.empty(2, cols, dtype=torch.float32, device=x.device)
+        at = dw.data_ptr()
+        self._check(self.lib.fs_layer_norm_grad(self.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), g,
+                                                FS_F32 if gamma is None else _DTYPES[gamma.dtype], stat.data_ptr(), dy.data_ptr(), _ld(dy),
+                                                dx.data_ptr(), cols, at, at + 4 * cols), "fs_layer_norm_grad")
+        return dx, dw[0], dw[1]
+
     def fs_points_keep(self, prob: Problem) -> None:
         """Declare the clouds of `prob` unchanged until fs_points_release: later calls reuse their derived copies."""
         self._check(self.lib.fs_points_keep(self.h, ctypes.byref(prob.c)), "fs_points_keep")
@@ -369,6 +515,79 @@ class Context:
         self._check(self.lib.fs_profile_read(self.h, ctypes.byref(avg), ctypes.byref(cnt),
                                              ctypes.byref(pairs)), "fs_profile_read")
         return avg.value, cnt.value, pairs.value
+
+
+class AdamW:
+    """AdamW over many tensors in one call of the library (``fs_adamw``): the weights are updated in place.
+
+    ``state_bits`` 8 keeps m and sqrt(v) as float8 codes under a scale for every 256 weights.  ``master``: float copies of bf16
+    weights.  The state is made here unless it is given (``m``, ``v``, ``m_scale``, ``v_scale``, and ``step``, the steps already taken).
+    """
+
+    def __init__(self, ctx: Context, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
+                 state_bits: int = 32, master=None, m=None, v=None, m_scale=None, v_scale=None, step: int = 0, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits is 8 or 32")
+        self.ctx, self.params, self.step_count, self.seed = ctx, list(params), int(step), int(seed)
+        self.lr, self.betas, self.eps, self.weight_decay, self.state_bits = lr, betas, eps, weight_decay, state_bits
+        if not self.params:
+            raise ValueError("no weights")
+        self.p_dtype = self.params[0].dtype
+        if self.p_dtype not in _DTYPES:
+            raise TypeError("weights must be float32 or bfloat16")
+        kind = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+
+        def made(given, dtype, count, fill):
+            if given is None:
+                return [torch.full((count(p),), fill, dtype=torch.float32, device=p.device).to(dtype) for p in self.params]
+            if len(given) != len(self.params):
+                raise ValueError("as many state tensors as weights")
+            for t, p in zip(given, self.params):
+                if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() != count(p):
+                    raise TypeError("a state tensor does not fit its weights")
+            return list(given)
+
+        for p in self.params:
+            if not p.is_cuda or p.dtype != self.p_dtype or not p.is_contiguous():
+                raise TypeError("weights must be contiguous GPU tensors of one type")
+        self.m = made(m, kind, lambda p: p.numel(), 0.0)
+        self.v = made(v, kind, lambda p: p.numel(), 0.0)
+        self.m_scale = self.v_scale = self.master = None
+        if state_bits == 8:
+            self.m_scale = made(m_scale, torch.float32, lambda p: (p.numel() + 255) // 256, 1.0)
+            self.v_scale = made(v_scale, torch.float32, lambda p: (p.numel() + 255) // 256, 1.0)
+        if master is not None:
+            self.master = made(master, torch.float32, lambda p: p.numel(), 0.0)
+        self._table = (FsAdamwTensor * len(self.params))()
+        lists = ((self.params, "p"), (self.m, "m"), (self.v, "v"), (self.m_scale, "m_scale"), (self.v_scale, "v_scale"), (self.master, "master"))
+        for tensors, field in lists:
+            for entry, t in zip(self._table, tensors or ()):
+                setattr(entry, field, t.data_ptr())
+        for entry, p in zip(self._table, self.params):
+            entry.n = p.numel()
+        self._args = FsAdamwArgs(p_dtype=_DTYPES[self.p_dtype], state_bits=state_bits)
+
+    def step(self, grads, grad_scale: Optional[torch.Tensor] = None) -> None:
+        """One step with these gradients (one type, contiguous, in the order of the weights).  ``grad_scale``: a float32 GPU scalar
+        that they are multiplied by."""
+        if len(grads) != len(self.params):
+            raise ValueError("as many gradients as weights")
+        kind = grads[0].dtype
+        if kind not in _DTYPES:
+            raise TypeError("gradients must be float32 or bfloat16")
+        for entry, g in zip(self._table, grads):
+            if not g.is_cuda or g.dtype != kind or not g.is_contiguous() or g.numel() != entry.n:
+                raise TypeError("a gradient does not fit its weights")
+            entry.g = g.data_ptr()
+        a = self._args
+        a.lr, (a.beta1, a.beta2), a.eps, a.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
+        a.step, a.g_dtype = self.step_count + 1, _DTYPES[kind]
+        a.seed = (self.seed + self.step_count + 1) & 0xFFFFFFFF
+        if grad_scale is not None and (not grad_scale.is_cuda or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+            raise TypeError("grad_scale must be a float32 GPU scalar")
+        a.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
+        self.ctx._check(self.ctx.lib.fs_adamw(self.ctx.h, ctypes.byref(a), self._table, len(self.params)), "fs_adamw")
+        self.step_count += 1
 
 
 def problem_from_workload(w, device="cuda:0") -> Problem:

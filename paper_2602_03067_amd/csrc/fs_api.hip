@@ -9,6 +9,7 @@
 #include <atomic>
 #include <new>
 
+#include "fs_attn.h"
 #include "fs_internal.h"
 
 namespace fs {
@@ -548,6 +549,134 @@ fs_status ensure_aux(Ctx *c, size_t need)
     c->aux_bytes = need;
     return FS_OK;
 }
+
+// ---- operators of a network trained on the losses ----------------------------------------------------
+
+constexpr const char *kHostOnly = "host-only context: arguments are valid, nothing was launched";
+
+// elements from the first to the last of a tensor of sets, rows and heads (0: none)
+int64_t heads_span(const fs_heads &t, int64_t batch, int64_t rows, int64_t heads, int64_t d)
+{
+    if (!batch || !rows || !heads) return 0;
+    return (batch - 1) * t.batch + (rows - 1) * t.row + (heads - 1) * t.head + d;
+}
+
+struct AttnCheck {
+    const fs_attn *a;
+    size_t es;
+    bool aligned = true;   // every row of every tensor starts at 16 bytes, and holds a whole number of them
+    struct Span {
+        const void *p;
+        size_t bytes;
+    } in[8];
+    int n_in = 0;
+};
+
+fs_status check_heads(Ctx *c, AttnCheck *k, const fs_heads *t, bool kv, bool out, const char *name)
+{
+    if (!t) return fail(c, FS_ERR_INVALID_ARG, "%s is NULL", name);
+    const fs_attn *a = k->a;
+    const int64_t rows = kv ? a->k_rows : a->q_rows, heads = kv ? a->kv_heads : a->q_heads;
+    const int64_t count[3] = {a->batch, rows, heads}, stride[3] = {t->batch, t->row, t->head};
+    if (!a->batch || !rows) return FS_OK;
+    if (!t->data) return fail(c, FS_ERR_INVALID_ARG, "%s is NULL", name);
+    if ((uintptr_t)t->data % k->es) return fail(c, FS_ERR_INVALID_ARG, "%s is not aligned to its type", name);
+    bool aligned = (uintptr_t)t->data % 16 == 0 && a->d * k->es % 16 == 0;
+    for (int i = 0; i < 3; ++i) {
+        if (stride[i] < 0 || stride[i] > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "%s: a stride is negative or beyond 2^40", name);
+        if (count[i] <= 1) continue;
+        if (out && stride[i] < a->d) return fail(c, FS_ERR_BAD_SHAPE, "%s: rows of an output overlap", name);
+        aligned = aligned && stride[i] * k->es % 16 == 0;
+    }
+    k->aligned = k->aligned && aligned;
+    const size_t bytes = (size_t)heads_span(*t, a->batch, rows, heads, a->d) * k->es;
+    if (!out) {
+        k->in[k->n_in++] = {t->data, bytes};
+    } else {
+        for (int i = 0; i < k->n_in; ++i)
+            if (overlap(t->data, bytes, k->in[i].p, k->in[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "%s overlaps an input", name);
+    }
+    return FS_OK;
+}
+
+fs_status check_attn(Ctx *c, AttnCheck *k, const fs_attn *a, AttnCall *call)
+{
+    if (!a) return fail(c, FS_ERR_INVALID_ARG, "attn is NULL");
+    if (a->dtype != FS_F32 && a->dtype != FS_BF16) return fail(c, FS_ERR_INVALID_ARG, "unknown dtype %d", (int)a->dtype);
+    if (a->causal != 0 && a->causal != 1) return fail(c, FS_ERR_INVALID_ARG, "causal is 0 or 1");
+    if (a->batch < 0 || a->q_rows < 0 || a->k_rows < 0 || a->q_heads <= 0 || a->kv_heads <= 0 || a->d <= 0)
+        return fail(c, FS_ERR_BAD_SHAPE, "sets and rows must not be negative, heads and d must be positive");
+    if (a->d > 128) return fail(c, FS_ERR_UNSUPPORTED, "d <= 128 coordinates per head are supported (got %lld)", (long long)a->d);
+    if (a->q_heads % a->kv_heads) return fail(c, FS_ERR_BAD_SHAPE, "kv_heads must divide q_heads");
+    const int64_t most = int64_t(1) << 24;
+    if (a->batch > most || a->q_rows > most || a->k_rows > most || a->q_heads > most) return fail(c, FS_ERR_BAD_SHAPE, "sets, rows and heads <= 2^24 are supported");
+    const int64_t group = a->q_heads / a->kv_heads, q_total = a->q_rows * group;
+    if (q_total > (int64_t(1) << 30) || a->batch * a->kv_heads > (int64_t(1) << 28) ||
+        (double)a->batch * a->kv_heads * (double)(q_total / 32 + a->k_rows / 32 + 2) > 1.0e9)
+        return fail(c, FS_ERR_BAD_SHAPE, "too many rows for one call");
+    if (!(a->scale > 0.0f) || !isfinite(a->scale)) return fail(c, FS_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (a->bias && a->bias_ld != 0 && a->bias_ld < a->k_rows) return fail(c, FS_ERR_BAD_SHAPE, "bias_ld is smaller than k_rows");
+    k->a = a;
+    k->es = a->dtype == FS_BF16 ? 2 : 4;
+    fs_status st;
+    if ((st = check_heads(c, k, &a->q, false, false, "q")) || (st = check_heads(c, k, &a->k, true, false, "k")) ||
+        (st = check_heads(c, k, &a->v, true, false, "v")))
+        return st;
+    if (a->bias && a->batch) k->in[k->n_in++] = {a->bias, (size_t)((a->batch - 1) * a->bias_ld + a->k_rows) * 4};
+    auto at = [](const fs_heads &t) { return HeadsAt{t.batch, t.row, t.head}; };
+    *call = AttnCall();
+    call->q = a->q.data;
+    call->k = a->k.data;
+    call->v = a->v.data;
+    call->sq = at(a->q);
+    call->sk = at(a->k);
+    call->sv = at(a->v);
+    call->q_len = a->q_len;
+    call->k_len = a->k_len;
+    call->bias = a->bias;
+    call->bias_ld = a->bias_ld;
+    call->batch = (int32_t)a->batch;
+    call->n = (int32_t)a->q_rows;
+    call->m = (int32_t)a->k_rows;
+    call->kv_heads = (int32_t)a->kv_heads;
+    call->group = (int32_t)group;
+    call->d = (int32_t)a->d;
+    call->causal = a->causal;
+    call->scale = a->scale;
+    call->splits = 1;
+    return FS_OK;
+}
+
+fs_status check_stat(Ctx *c, const float *stat, int64_t rows)
+{
+    if (!rows) return FS_OK;
+    if (!stat) return fail(c, FS_ERR_INVALID_ARG, "stat is NULL");
+    if ((uintptr_t)stat % 8) return fail(c, FS_ERR_INVALID_ARG, "stat must be aligned to 8 bytes");
+    return FS_OK;
+}
+
+fs_status check_rows(Ctx *c, const void *p, size_t es, int64_t rows, int64_t cols, int64_t ld, const char *name)
+{
+    if (ld < cols) return fail(c, FS_ERR_BAD_SHAPE, "%s: leading dimension smaller than cols", name);
+    if (ld > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "%s: leading dimension beyond 2^40", name);
+    if (rows && !p) return fail(c, FS_ERR_INVALID_ARG, "%s is NULL", name);
+    if ((uintptr_t)p % es) return fail(c, FS_ERR_INVALID_ARG, "%s is not aligned to its type", name);
+    return FS_OK;
+}
+
+fs_status check_norm(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, const void *beta,
+                     int32_t wtype)
+{
+    if (dtype != FS_F32 && dtype != FS_BF16) return fail(c, FS_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (wtype != FS_F32 && wtype != FS_BF16) return fail(c, FS_ERR_INVALID_ARG, "unknown wtype %d", (int)wtype);
+    if (rows < 0 || cols <= 0 || rows > (int64_t(1) << 30) || cols > (int64_t(1) << 24))
+        return fail(c, FS_ERR_BAD_SHAPE, "0 <= rows <= 2^30 and 1 <= cols <= 2^24 are supported");
+    const size_t es = dtype == FS_BF16 ? 2 : 4, ws = wtype == FS_BF16 ? 2 : 4;
+    if ((uintptr_t)gamma % ws || (uintptr_t)beta % ws) return fail(c, FS_ERR_INVALID_ARG, "gamma or beta is not aligned to its type");
+    return check_rows(c, x, es, rows, cols, ldx, "x");
+}
+
+size_t rows_bytes(int64_t rows, int64_t cols, int64_t ld, size_t es) { return rows ? (size_t)((rows - 1) * ld + cols) * es : 0; }
 
 }  // namespace
 }  // namespace fs
@@ -1279,6 +1408,195 @@ fs_status fs_points_release(fs_ctx *ctx)
     c->keep_on = false;
     c->kept_valid = false;
     return FS_OK;
+}
+
+fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, float *stat)
+{
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard device_guard(c);
+    if (!c) return FS_ERR_INVALID_ARG;
+    c->err.clear();
+    AttnCheck k;
+    AttnCall a;
+    fs_status st;
+    if ((st = check_attn(c, &k, attn, &a)) || (st = check_heads(c, &k, o, false, true, "o"))) return st;
+    const int64_t rows = attn->batch * attn->q_heads * attn->q_rows;
+    if ((st = check_stat(c, stat, rows))) return st;
+    for (int i = 0; i < k.n_in; ++i)
+        if (overlap(stat, (size_t)rows * 8, k.in[i].p, k.in[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "stat overlaps an input");
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!rows) return FS_OK;
+    a.o = o->data;
+    a.so = {o->batch, o->row, o->head};
+    a.stat = stat;
+    const bool f32 = attn->dtype == FS_F32;
+    const AttnPlan p = attn_plan(c, a, f32);
+    a.splits = p.splits;
+    if (p.splits > 1) {
+        Arena A;
+        const size_t part = A.take(p.part_bytes), ps = A.take(p.stat_bytes);
+        if ((st = ensure_aux(c, A.off))) return st;
+        a.part = (float *)(c->aux + part);
+        a.part_stat = (float *)(c->aux + ps);
+    }
+    return launch_attn(c, a, p, f32, k.aligned);
+}
+
+fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, const float *stat, const fs_heads *d_o, const fs_heads *dq,
+                            const fs_heads *dk, const fs_heads *dv, void *dbias, int64_t dbias_ld)
+{
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard device_guard(c);
+    if (!c) return FS_ERR_INVALID_ARG;
+    c->err.clear();
+    AttnCheck k;
+    AttnCall a;
+    fs_status st;
+    if ((st = check_attn(c, &k, attn, &a)) || (st = check_heads(c, &k, o, false, false, "o")) ||
+        (st = check_heads(c, &k, d_o, false, false, "d_o")))
+        return st;
+    const int64_t rows = attn->batch * attn->q_heads * attn->q_rows;
+    if ((st = check_stat(c, stat, rows))) return st;
+    k.in[k.n_in++] = {stat, (size_t)rows * 8};
+    if ((st = check_heads(c, &k, dq, false, true, "dq")) || (st = check_heads(c, &k, dk, true, true, "dk")) ||
+        (st = check_heads(c, &k, dv, true, true, "dv")))
+        return st;
+    if (dbias) {
+        if (!attn->bias) return fail(c, FS_ERR_INVALID_ARG, "dbias without bias");
+        if (attn->bias_ld == 0 && attn->batch > 1) return fail(c, FS_ERR_UNSUPPORTED, "dbias of a bias that the sets share");
+        if (dbias_ld < attn->k_rows || dbias_ld > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "dbias_ld is smaller than k_rows, or beyond 2^40");
+        if ((uintptr_t)dbias % k.es) return fail(c, FS_ERR_INVALID_ARG, "dbias is not aligned to its type");
+        for (int i = 0; i < k.n_in; ++i)
+            if (overlap(dbias, rows_bytes(attn->batch, attn->k_rows, dbias_ld, k.es), k.in[i].p, k.in[i].bytes))
+                return fail(c, FS_ERR_INVALID_ARG, "dbias overlaps an input");
+    }
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!attn->batch) return FS_OK;
+    a.o = o->data;
+    a.so = {o->batch, o->row, o->head};
+    a.d_o = d_o->data;
+    a.s_do = {d_o->batch, d_o->row, d_o->head};
+    a.stat = const_cast<float *>(stat);
+    a.dq = dq->data;
+    a.sdq = {dq->batch, dq->row, dq->head};
+    a.dk = dk->data;
+    a.sdk = {dk->batch, dk->row, dk->head};
+    a.dv = dv->data;
+    a.sdv = {dv->batch, dv->row, dv->head};
+    a.dbias = dbias;
+    a.dbias_ld = dbias_ld;
+    const bool f32 = attn->dtype == FS_F32;
+    const AttnGradPlan p = attn_grad_plan(c, a, f32);
+    Arena A;
+    A.take(p.delta_bytes);
+    A.take(p.dq_bytes);
+    A.take(p.dkv_bytes);
+    A.take(p.dbias_bytes);
+    if ((st = ensure_aux(c, A.off))) return st;
+    return launch_attn_grad(c, a, p, c->aux, f32, k.aligned);
+}
+
+fs_status fs_layer_norm(fs_ctx *ctx, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma,
+                        const void *beta, int32_t wtype, float eps, void *y, int64_t ldy, float *stat)
+{
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard device_guard(c);
+    if (!c) return FS_ERR_INVALID_ARG;
+    c->err.clear();
+    fs_status st;
+    if ((st = check_norm(c, x, dtype, rows, cols, ldx, gamma, beta, wtype))) return st;
+    const size_t es = dtype == FS_BF16 ? 2 : 4, ws = wtype == FS_BF16 ? 2 : 4;
+    if ((st = check_rows(c, y, es, rows, cols, ldy, "y"))) return st;
+    if (!(eps >= 0.0f) || !isfinite(eps)) return fail(c, FS_ERR_BAD_EPS, "eps must be finite and not negative");
+    if (stat && (st = check_stat(c, stat, rows))) return st;
+    const struct {
+        const void *p;
+        size_t bytes;
+    } in[] = {{x, rows_bytes(rows, cols, ldx, es)}, {gamma, (size_t)cols * ws}, {beta, (size_t)cols * ws}};
+    for (const auto &i : in)
+        if (overlap(y, rows_bytes(rows, cols, ldy, es), i.p, i.bytes) || overlap(stat, (size_t)rows * 8, i.p, i.bytes))
+            return fail(c, FS_ERR_INVALID_ARG, "an output overlaps an input");
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!rows) return FS_OK;
+    return launch_norm(c, x, dtype, rows, cols, ldx, gamma, beta, wtype, eps, y, ldy, stat);
+}
+
+fs_status fs_layer_norm_grad(fs_ctx *ctx, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma,
+                             int32_t wtype, const float *stat, const void *dy, int64_t lddy, void *dx, int64_t lddx, float *dgamma,
+                             float *dbeta)
+{
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard device_guard(c);
+    if (!c) return FS_ERR_INVALID_ARG;
+    c->err.clear();
+    fs_status st;
+    if ((st = check_norm(c, x, dtype, rows, cols, ldx, gamma, nullptr, wtype))) return st;
+    const size_t es = dtype == FS_BF16 ? 2 : 4, ws = wtype == FS_BF16 ? 2 : 4;
+    if ((st = check_rows(c, dy, es, rows, cols, lddy, "dy")) || (st = check_stat(c, stat, rows))) return st;
+    if (dx && (st = check_rows(c, dx, es, rows, cols, lddx, "dx"))) return st;
+    const size_t xb = rows_bytes(rows, cols, ldx, es), yb = rows_bytes(rows, cols, lddy, es), gb = rows_bytes(rows, cols, lddx, es);
+    const bool in_place = dx && dx == dy && lddx == lddy;
+    const struct {
+        const void *p;
+        size_t bytes;
+    } in[] = {{x, xb}, {gamma, (size_t)cols * ws}, {stat, (size_t)rows * 8}, {dy, yb}}, out[] = {{dx, gb}, {dgamma, (size_t)cols * 4}, {dbeta, (size_t)cols * 4}};
+    for (const auto &i : in)
+        for (const auto &q : out)
+            if (overlap(q.p, q.bytes, i.p, i.bytes) && !(in_place && q.p == dx && i.p == dy))
+                return fail(c, FS_ERR_INVALID_ARG, "an output overlaps an input");
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!dx && !dgamma && !dbeta) return FS_OK;
+    float *part = nullptr;
+    if (dgamma || dbeta) {
+        if ((st = ensure_aux(c, (size_t)norm_grad_blocks(c, rows) * 2 * cols * 4))) return st;
+        part = (float *)c->aux;
+    }
+    return launch_norm_grad(c, x, dtype, rows, cols, ldx, gamma, wtype, stat, dy, lddy, dx, lddx, dgamma, dbeta, part);
+}
+
+fs_status fs_adamw(fs_ctx *ctx, const fs_adamw_args *args, const fs_adamw_tensor *tensors, int32_t count)
+{
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard device_guard(c);
+    if (!c) return FS_ERR_INVALID_ARG;
+    c->err.clear();
+    if (!args || (!tensors && count > 0)) return fail(c, FS_ERR_INVALID_ARG, "args or tensors is NULL");
+    if (count < 0) return fail(c, FS_ERR_BAD_SHAPE, "count is negative");
+    const fs_adamw_args *a = args;
+    for (int32_t t : {a->p_dtype, a->g_dtype})
+        if (t != FS_F32 && t != FS_BF16) return fail(c, FS_ERR_INVALID_ARG, "unknown dtype %d", (int)t);
+    if (a->state_bits != 32 && a->state_bits != 8) return fail(c, FS_ERR_UNSUPPORTED, "states of 32 or 8 bits (got %d)", (int)a->state_bits);
+    auto fine = [](double v) { return v >= 0.0 && isfinite(v); };
+    if (!fine(a->lr) || !fine(a->eps) || !fine(a->weight_decay) || !(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0))
+        return fail(c, FS_ERR_INVALID_ARG, "lr, eps, weight_decay must be finite and not negative, betas in [0, 1)");
+    if (a->step < 1) return fail(c, FS_ERR_INVALID_ARG, "step counts from 1");
+    bool master = false, some = false;
+    for (int32_t i = 0; i < count; ++i) {
+        const fs_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || t.n > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "tensor %d: 0 <= n <= 2^40", (int)i);
+        if (!t.n) continue;
+        const bool q8 = a->state_bits == 8;
+        if (!t.p || !t.g || !t.m || !t.v || (q8 && (!t.m_scale || !t.v_scale))) return fail(c, FS_ERR_INVALID_ARG, "tensor %d: a pointer is NULL", (int)i);
+        if (some && (t.master != nullptr) != master) return fail(c, FS_ERR_INVALID_ARG, "tensor %d: masters for all tensors or for none", (int)i);
+        master = t.master != nullptr;
+        some = true;
+        if (master && a->p_dtype != FS_BF16) return fail(c, FS_ERR_UNSUPPORTED, "masters are for bf16 weights");
+        const size_t n = (size_t)t.n, sc = (n + 255) / 256 * 4;
+        const struct {
+            const void *p;
+            size_t bytes, es;
+        } all[] = {{t.g, n * (a->g_dtype == FS_BF16 ? 2 : 4), a->g_dtype == FS_BF16 ? 2u : 4u}, {t.p, n * (a->p_dtype == FS_BF16 ? 2 : 4), a->p_dtype == FS_BF16 ? 2u : 4u},
+                   {t.master, n * 4, 4}, {t.m, n * (q8 ? 1 : 4), q8 ? 1u : 4u}, {t.v, n * (q8 ? 1 : 4), q8 ? 1u : 4u},
+                   {q8 ? t.m_scale : nullptr, sc, 4}, {q8 ? t.v_scale : nullptr, sc, 4}};
+        for (size_t u = 0; u < sizeof all / sizeof *all; ++u) {
+            if ((uintptr_t)all[u].p % all[u].es) return fail(c, FS_ERR_INVALID_ARG, "tensor %d: a pointer is not aligned to its type", (int)i);
+            for (size_t w = 0; w < u; ++w)
+                if (overlap(all[u].p, all[u].bytes, all[w].p, all[w].bytes)) return fail(c, FS_ERR_INVALID_ARG, "tensor %d: its arrays overlap", (int)i);
+        }
+    }
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!some) return FS_OK;
+    return launch_adamw(c, a, tensors, count, master);
 }
 
 fs_status fs_debug_set(fs_ctx *ctx, const char *key, int64_t value)

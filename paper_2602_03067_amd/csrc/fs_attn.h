@@ -1,0 +1,214 @@
+// What the forward and the backward kernels of attention share: operands of the matrix cores, tiles in LDS, and the
+// description of a call.
+//
+// Both element types go through 32 x 32 products whose operands are 16 bytes a lane: eight bf16 (one v_mfma_f32_32x32x16_bf16)
+// or four floats (four v_mfma_f32_32x32x2_f32).  Lane l = 32 h + c holds row (column) c of the operand and the contraction
+// indices kStep t + (kStep / 2) h + 0, 1, ..; register r of a product holds row 8 (r / 4) + 4 h + r % 4 of column c.  So the
+// registers of one product, a step's share at a time, are the second operand of the next one as they stand, if its first operand
+// takes the rows in that order: probabilities never pass through LDS.
+#pragma once
+
+#include "fs_internal.h"
+
+namespace fs {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> struct Mma;
+
+template <> struct Mma<__bf16> {
+    using Frag = bf16x8;
+    static constexpr int kStep = 16;    // contraction indices of a fragment
+    static constexpr int kPiece = 8;    // elements of 16 bytes
+    static __device__ inline f32x16 mma(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    // registers kStep / 2 * t .. of a product as an operand
+    static __device__ inline Frag pack(const f32x16 &v, int t)
+    {
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (__bf16)v[8 * t + j];
+        return f;
+    }
+    static __device__ inline float load(const __bf16 *p) { return (float)*p; }
+};
+
+template <> struct Mma<float> {
+    using Frag = f32x4;
+    static constexpr int kStep = 8;
+    static constexpr int kPiece = 4;
+    static __device__ inline f32x16 mma(Frag a, Frag b, f32x16 c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ inline Frag pack(const f32x16 &v, int t)
+    {
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = v[4 * t + j];
+        return f;
+    }
+    static __device__ inline float load(const float *p) { return *p; }
+};
+
+// A tile of rows in LDS, DP elements each (zero beyond d).  16-byte pieces are permuted within their row so that the lanes of a
+// fragment read, which take one piece each of 32 consecutive rows, meet in as few banks as there are.
+template <typename T, int DP> struct Tile {
+    static constexpr int kRow = DP * (int)sizeof(T);   // bytes
+    static constexpr int kPieces = kRow / 16;
+    static __device__ inline int swz(int row) { return kPieces % 8 == 0 ? row & 7 : (row >> 1) & 3; }
+    static __device__ inline int at(int row, int piece) { return row * kRow + ((piece ^ swz(row)) << 4); }
+    // operand with the tile's rows as rows: step t of the contraction over coordinates
+    static __device__ inline typename Mma<T>::Frag rows(const char *lds, int row0, int t, int lane)
+    {
+        return *(const typename Mma<T>::Frag *)(lds + at(row0 + (lane & 31), 2 * t + (lane >> 5)));
+    }
+    // operand with coordinates 32 db .. 32 db + 31 as rows: step t of the contraction over the 32 rows from row0 on, in the order
+    // in which a product's registers hold them
+    static __device__ inline typename Mma<T>::Frag cols(const char *lds, int row0, int t, int db, int lane)
+    {
+        if constexpr (sizeof(T) == 2) {
+            // sixteen lanes read 4 rows x 16 coordinates, eight bytes each, and get a coordinate each: its four rows
+            const int i = lane & 15, piece = 4 * db + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+            const int r = row0 + 16 * t + 4 * (lane >> 5) + (i >> 2);
+            using P = __attribute__((address_space(3))) s16x4 *;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds_offset(lds) + at(r, piece) + (i & 1) * 8));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds_offset(lds) + at(r + 8, piece) + (i & 1) * 8));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            f32x4 f;
+            const int c = 32 * db + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                f[j] = *(const float *)(lds + at(row0 + 8 * t + 4 * (lane >> 5) + j, c >> 2) + (c & 3) * 4);
+            return f;
+        }
+    }
+    static __device__ inline unsigned lds_offset(const char *p)
+    {
+        return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+    }
+};
+
+// 16 bytes of a row: elements piece * kPiece .. of d, zero beyond.  ALN: rows are 16-byte aligned and d is a multiple of kPiece.
+template <typename T, bool ALN> __device__ inline uint4 load_piece(const T *row, int piece, int d)
+{
+    constexpr int E = Mma<T>::kPiece;
+    if constexpr (ALN) {
+        return piece * E < d ? *(const uint4 *)(row + piece * E) : make_uint4(0, 0, 0, 0);
+    } else {
+        union {
+            uint4 u;
+            T e[E];
+        } v;
+        v.u = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (piece * E + j < d) v.e[j] = row[piece * E + j];
+        return v.u;
+    }
+}
+
+// four coordinates each of a product's column: coordinates col + 8 u + 0 .. 3 from registers 4 u ..
+template <typename T, bool ALN> __device__ inline void store_column(T *row, const f32x16 &v, float f, int col, int d)
+{
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (ALN) {   // (d is a multiple of four, and so is col)
+            if (col + 8 * u < d) {
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                T4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = (T)(v[4 * u + j] * f);
+                *(T4 *)(row + col + 8 * u) = w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (col + 8 * u + j < d) row[col + 8 * u + j] = (T)(v[4 * u + j] * f);
+        }
+    }
+}
+
+// where the rows of one tensor lie: element strides of sets (batch), rows and heads
+struct HeadsAt {
+    int64_t batch, row, head;
+};
+
+struct AttnCall {
+    const void *q, *k, *v;
+    HeadsAt sq, sk, sv;
+    void *o;                     // forward: written; backward: read
+    HeadsAt so;
+    float *stat;                 // [batch][heads][n][2]: the row's largest score, and its sum of exponentials below that
+    const void *d_o;             // backward
+    HeadsAt s_do;
+    void *dq, *dk, *dv, *dbias;
+    HeadsAt sdq, sdk, sdv;
+    int64_t dbias_ld;
+    float *delta;                // backward: [batch][kv head][packed row] <do, o>
+    const int32_t *q_len, *k_len;
+    const float *bias;
+    int64_t bias_ld;
+    int32_t batch, n, m, kv_heads, group, d, causal;
+    float scale;
+    // Splits of the streamed side; more than one: partial results, merged afterwards
+    int32_t splits;
+    float *part, *part_stat;
+    float *dbias_part;           // backward: [split][batch][kv head][key]
+};
+
+// The heads that share keys are taken together: packed row r of (set, kv head) is query r / group of head kv_head * group + r % group.
+struct Packed {
+    int q, g;
+};
+__device__ inline Packed unpack(int r, int group)
+{
+    if (group == 1) return {r, 0};
+    const int q = r / group;
+    return {q, r - q * group};
+}
+
+// Workgroups that share an XCD's L2 (ids equal mod 8) take consecutive work.
+__device__ inline int xcd_order(int id, int total)
+{
+    const int x = id & 7, j = id >> 3, per = total >> 3, more = total & 7;
+    return x * per + (x < more ? x : more) + j;
+}
+
+// how a forward pass is launched
+struct AttnPlan {
+    int waves, splits;
+    int64_t grid;
+    size_t part_bytes, stat_bytes;
+};
+AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32);
+fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bool aligned);
+
+// ... and a backward pass: rows' side (dq) and keys' side (dk, dv)
+struct AttnGradPlan {
+    int q_splits, k_splits;
+    int64_t q_grid, k_grid;
+    size_t delta_bytes, dq_bytes, dkv_bytes, dbias_bytes;
+};
+AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32);
+// `ws`: the bytes of the plan, each piece rounded up to 256
+fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool f32, bool aligned);
+
+__device__ inline float across_halves_max(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)p[0]), __builtin_bit_cast(float, (unsigned)p[1]));
+}
+__device__ inline float across_halves_sum(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
+}
+
+}  // namespace fs

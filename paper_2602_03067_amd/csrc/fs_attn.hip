@@ -1,0 +1,288 @@
+// Softmax attention, forward:  o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - m_i) / l_i,  s_ij = scale <q_i, k_j> + bias_j,
+// over the keys j that row i may see.  One pass over the keys with the running maximum and sum of every row; scores and
+// probabilities stay in registers: a wave holds 32 rows as columns, S^T = K Q^T, and its registers are the operand of
+// O^T += V^T P^T (fs_attn.h).
+#include <algorithm>
+
+#include "fs_attn.h"
+
+namespace fs {
+namespace {
+
+constexpr float kLog2eF = 1.44269504088896340736f;
+// Probabilities are taken below a reference that follows the row's maximum at a distance of at most 2^8: the accumulators are
+// rescaled only where the maximum has grown by more.  Sums stay far inside a float, and a bf16 probability has the same
+// relative rounding at any size.
+constexpr float kSlack = 8.0f;
+
+template <typename T, int DP, int KT, int WAVES, bool BIAS, bool ALN>
+__global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
+{
+    using M = Mma<T>;
+    using Frag = typename M::Frag;
+    using TL = Tile<T, DP>;
+    constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
+    constexpr int kTile = KT * TL::kRow, NPC = KT * TL::kPieces / NT;
+    static_assert(KT * TL::kPieces % NT == 0, "");
+    __shared__ __align__(16) char lds[4 * kTile];
+    __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int split = id % c.splits;
+    id /= c.splits;
+    const int blk = blocks - 1 - id % blocks;   // (causal: the long ones first)
+    id /= blocks;
+    const int hk = id % c.kv_heads, b = id / c.kv_heads;
+
+    const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
+    const int q_len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
+    const int r = blk * 32 * WAVES + wave * 32 + (lane & 31);
+    const Packed pk = unpack(r, c.group);
+    const bool live = r < rows && pk.q < q_len;
+    // keys that this row sees: 0 .. limit - 1
+    const int limit = !live ? 0 : c.causal ? min(k_len, max(0, pk.q + k_len - q_len + 1)) : k_len;
+    const int last_q = min((min(rows, (blk + 1) * 32 * WAVES) - 1) / c.group, q_len - 1);
+    const int hi = last_q < blk * 32 * WAVES / c.group ? 0 : c.causal ? min(k_len, max(0, last_q + k_len - q_len + 1)) : k_len;
+    const int tiles = (hi + KT - 1) / KT, per = (tiles + c.splits - 1) / c.splits;
+    const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
+
+    const T *kp = (const T *)c.k + b * c.sk.batch + hk * c.sk.head;
+    const T *vp = (const T *)c.v + b * c.sv.batch + hk * c.sv.head;
+    const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
+
+    Frag q[NS];
+    {
+        const T *row = (const T *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + (hk * c.group + pk.g) * c.sq.head;
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+            q[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(row, 2 * t + half, c.d) : make_uint4(0, 0, 0, 0));
+    }
+
+    uint4 kr[NPC], vr[NPC];
+    float br = 0.0f;
+    auto fetch = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            const int p = tid + i * NT, row = p / TL::kPieces, pc = p % TL::kPieces, key = tile * KT + row;
+            const bool there = key < k_len && (!BIAS || bp[key] != -INFINITY);   // what removed keys hold does not matter
+            kr[i] = there ? load_piece<T, ALN>(kp + (int64_t)key * c.sk.row, pc, c.d) : make_uint4(0, 0, 0, 0);
+            vr[i] = there ? load_piece<T, ALN>(vp + (int64_t)key * c.sv.row, pc, c.d) : make_uint4(0, 0, 0, 0);
+        }
+        if (BIAS && tid < KT) br = tile * KT + tid < k_len ? bp[tile * KT + tid] : -INFINITY;
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
+            *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
+            *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
+        }
+        if (BIAS && tid < KT) lbias[buf][tid] = br;
+    };
+
+    f32x16 o[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) o[i] = (f32x16)(0.0f);
+    // units of the running values: without bias the products <q, k>, with it the scores
+    const float unit = BIAS ? kLog2eF : c.scale * kLog2eF;
+    // exp2((s - ref) unit), the difference first: a bias of the type's lowest value times log2 e would leave the type, and full
+    // precision is not to lose an ulp of the larger of the two.  In bf16 without bias one fma does.
+    constexpr bool kDiff = BIAS || sizeof(T) == 4;
+    float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
+
+    if (t0 < t1) {
+        fetch(t0);
+        put(0);
+    }
+    __syncthreads();
+    for (int tile = t0; tile < t1; ++tile) {
+        const int buf = (tile - t0) & 1;
+        const char *lk = lds + 2 * buf * kTile, *lv = lk + kTile;
+        if (tile + 1 < t1) fetch(tile + 1);
+
+        f32x16 s[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            s[nb] = (f32x16)(0.0f);
+#pragma unroll
+            for (int t = 0; t < NS; ++t) s[nb] = M::mma(TL::rows(lk, nb * 32, t, lane), q[t], s[nb]);
+        }
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 w = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * g + 4 * half];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], c.scale, w[j]);
+                }
+        }
+        const int base = tile * KT + 4 * half;
+        if (__any(limit < (tile + 1) * KT)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[nb][i] = base + nb * 32 + 8 * (i / 4) + i % 4 < limit ? s[nb][i] : -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[nb][i]);
+        mx = across_halves_max(mx);
+        top = fmaxf(top, mx);
+        if (__any((mx - ref) * unit > kSlack)) {   // (the first keys of a row: from minus infinity)
+            const float next = fmaxf(ref, mx), f = next == ref ? 1.0f : __builtin_amdgcn_exp2f((ref - next) * unit);
+            ref = next;
+            sum *= f;
+#pragma unroll
+            for (int i = 0; i < ND; ++i) o[i] *= f;
+        }
+        const float safe = ref == -INFINITY ? 0.0f : ref, off = safe * unit;
+        float part = 0.0f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = kDiff ? __builtin_amdgcn_exp2f((s[nb][i] - safe) * unit)
+                                      : __builtin_amdgcn_exp2f(fmaf(s[nb][i], unit, -off));
+                s[nb][i] = e;
+                part += e;
+            }
+        sum += part;
+        // O^T += V^T P^T; a bf16 probability is rounded to 2^-9 of itself, its row's sum takes it unrounded
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int t = 0; t < NF; ++t) {
+                const Frag p = M::pack(s[nb], t);
+#pragma unroll
+                for (int i = 0; i < ND; ++i) o[i] = M::mma(TL::cols(lv, nb * 32, t, i, lane), p, o[i]);
+            }
+        if (tile + 1 < t1) put(buf ^ 1);
+        __syncthreads();
+    }
+
+    sum = across_halves_sum(sum);
+    if (r >= rows) return;
+    const float st = BIAS ? 1.0f : c.scale;   // the running values as scores
+    if (c.splits > 1) {
+        const int64_t at = ((int64_t)split * c.batch * c.kv_heads + (int64_t)b * c.kv_heads + hk) * rows + r;
+        float *po = c.part + at * DP + 4 * half;
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(f32x4 *)(po + 32 * i + 8 * g) = f32x4{o[i][4 * g], o[i][4 * g + 1], o[i][4 * g + 2], o[i][4 * g + 3]};
+        if (half == 0) *(f32x4 *)(c.part_stat + at * 4) = f32x4{top * st, ref * st, sum, 0.0f};
+        return;
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    T *out = (T *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + (hk * c.group + pk.g) * c.so.head;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) store_column<T, ALN>(out, o[i], inv, 32 * i + 4 * half, c.d);
+    if (half == 0) {
+        const int64_t at = (((int64_t)b * c.kv_heads + hk) * c.group + pk.g) * c.n + pk.q;
+        // the sum below the maximum itself
+        const float safe = ref == -INFINITY ? 0.0f : ref;
+        *(float2 *)(c.stat + 2 * at) = make_float2(top * st, sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f((safe - top) * unit));
+    }
+}
+
+// Merge of the splits: a wave takes a packed row, a lane two coordinates.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_join(const AttnCall c)
+{
+    const int rows = c.n * c.group, lane = threadIdx.x & 63;
+    const int64_t total = (int64_t)c.batch * c.kv_heads * rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= total) return;
+    float top = -INFINITY;
+    for (int s = 0; s < c.splits; ++s) top = fmaxf(top, c.part_stat[(s * total + at) * 4]);
+    const float safe = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, acc[(DP + 63) / 64] = {};
+    for (int s = 0; s < c.splits; ++s) {
+        const f32x4 st = *(const f32x4 *)(c.part_stat + (s * total + at) * 4);
+        if (st[1] == -INFINITY) continue;   // no key of this split
+        const float f = __builtin_amdgcn_exp2f((st[1] - safe) * kLog2eF);
+        sum = fmaf(st[2], f, sum);
+#pragma unroll
+        for (int i = 0; i < (DP + 63) / 64; ++i)
+            if (lane + 64 * i < DP) acc[i] = fmaf(c.part[(s * total + at) * DP + lane + 64 * i], f, acc[i]);
+    }
+    const int64_t bh = at / rows;
+    const Packed pk = unpack((int)(at - bh * rows), c.group);
+    const int hk = (int)(bh % c.kv_heads), b = (int)(bh / c.kv_heads);
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    T *out = (T *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + (hk * c.group + pk.g) * c.so.head;
+#pragma unroll
+    for (int i = 0; i < (DP + 63) / 64; ++i)
+        if (lane + 64 * i < c.d) out[lane + 64 * i] = (T)(acc[i] * inv);
+    if (lane == 0) *(float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q)) = make_float2(top, sum);
+}
+
+template <typename T, int DP, int KT, int WAVES>
+fs_status run(Ctx *c, const AttnCall &a, bool aligned, int64_t grid)
+{
+    if (a.bias) {
+        if (aligned) k_attn<T, DP, KT, WAVES, true, true><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
+        else k_attn<T, DP, KT, WAVES, true, false><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
+    } else {
+        if (aligned) k_attn<T, DP, KT, WAVES, false, true><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
+        else k_attn<T, DP, KT, WAVES, false, false><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
+    }
+    if (a.splits > 1) {
+        const int64_t total = (int64_t)a.batch * a.kv_heads * a.n * a.group;
+        k_attn_join<T, DP><<<(unsigned)ceil_div(total, 4), 256, 0, c->stream>>>(a);
+    }
+    FS_HIP(c, hipGetLastError());
+    return FS_OK;
+}
+
+template <typename T>
+fs_status by_width(Ctx *c, const AttnCall &a, bool aligned, int waves, int64_t grid)
+{
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32;
+    const int dp = (a.d + 31) / 32;
+    if (waves == 1) {
+        switch (dp) {
+        case 1: return run<T, 32, 32, 1>(c, a, aligned, grid);
+        case 2: return run<T, 64, 32, 1>(c, a, aligned, grid);
+        case 3: return run<T, 96, 32, 1>(c, a, aligned, grid);
+        default: return run<T, 128, 32, 1>(c, a, aligned, grid);
+        }
+    }
+    switch (dp) {
+    case 1: return run<T, 32, KT, 4>(c, a, aligned, grid);
+    case 2: return run<T, 64, KT, 4>(c, a, aligned, grid);
+    case 3: return run<T, 96, KT, 4>(c, a, aligned, grid);
+    default: return run<T, 128, KT, 4>(c, a, aligned, grid);
+    }
+}
+
+}  // namespace
+
+AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
+{
+    AttnPlan p;
+    const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads;
+    p.waves = rows <= 32 ? 1 : 4;
+    const int kt = p.waves == 1 || f32 ? 32 : 64;
+    const int64_t blocks = ceil_div(rows, 32 * p.waves) * heads, tiles = ceil_div(a.m, kt);
+    const int64_t want = (int64_t)c->num_cu * (p.waves == 1 ? 4 : 2);
+    p.splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(blocks, 1), tiles / 4));
+    p.grid = blocks * p.splits;
+    const int64_t dp = round_up(a.d, 32), total = heads * rows * p.splits;
+    p.part_bytes = p.splits > 1 ? (size_t)total * dp * 4 : 0;
+    p.stat_bytes = p.splits > 1 ? (size_t)total * 16 : 0;
+    return p;
+}
+
+fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bool aligned)
+{
+    return f32 ? by_width<float>(c, a, aligned, p.waves, p.grid) : by_width<__bf16>(c, a, aligned, p.waves, p.grid);
+}
+
+}  // namespace fs

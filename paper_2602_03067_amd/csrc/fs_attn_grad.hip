@@ -1,0 +1,465 @@
+// Backward pass of attention.  With p_ij recomputed from the row statistics of the forward pass and D_i = <do_i, o_i>,
+//   dv_j = sum_i p_ij do_i      ds_ij = p_ij (<do_i, v_j> - D_i)      dq_i = scale sum_j ds_ij k_j
+//   dk_j = scale sum_i ds_ij q_i      dbias_j = sum_i ds_ij
+// (sums over i run over all heads that share the keys).  Two passes that both recompute the scores, one whose waves hold 32
+// rows and stream keys (dq, and D on the way), one whose waves hold 32 keys and stream rows (dk, dv): seven products of
+// n m d instead of five, but nothing is added by atomics, so results do not depend on an order, and no n x m matrix is stored.
+#include <algorithm>
+
+#include "fs_attn.h"
+
+namespace fs {
+namespace {
+
+constexpr float kLog2eF = 1.44269504088896340736f;
+
+// What turns a score into a probability: exp2((s - m) log2 e - off), m the row's largest score (DIFF: the difference first, see
+// k_attn), or exp2(s log2 e - off) with m in off.  A row that sees no key has off = infinity.
+struct RowStat {
+    float m, off;
+};
+template <bool DIFF> __device__ inline RowStat row_stat(float top, float sum)
+{
+    if (!(sum > 0.0f) && sum == sum) return {0.0f, INFINITY};
+    const float lg = __builtin_amdgcn_logf(sum);
+    return DIFF ? RowStat{top, lg} : RowStat{0.0f, fmaf(top, kLog2eF, lg)};
+}
+
+template <typename T, int DP, int KT, int WAVES, bool BIAS, bool ALN>
+__global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
+{
+    using M = Mma<T>;
+    using Frag = typename M::Frag;
+    using TL = Tile<T, DP>;
+    constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
+    constexpr int kTile = KT * TL::kRow, NPC = KT * TL::kPieces / NT;
+    constexpr bool kDiff = BIAS || sizeof(T) == 4;
+    static_assert(KT * TL::kPieces % NT == 0, "");
+    __shared__ __align__(16) char lds[4 * kTile];
+    __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int split = id % c.splits;
+    id /= c.splits;
+    const int blk = blocks - 1 - id % blocks;
+    id /= blocks;
+    const int hk = id % c.kv_heads, b = id / c.kv_heads;
+
+    const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
+    const int q_len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
+    const int r = blk * 32 * WAVES + wave * 32 + (lane & 31);
+    const Packed pk = unpack(r, c.group);
+    const bool live = r < rows && pk.q < q_len;
+    const int limit = !live ? 0 : c.causal ? min(k_len, max(0, pk.q + k_len - q_len + 1)) : k_len;
+    const int last_q = min((min(rows, (blk + 1) * 32 * WAVES) - 1) / c.group, q_len - 1);
+    const int hi = last_q < blk * 32 * WAVES / c.group ? 0 : c.causal ? min(k_len, max(0, last_q + k_len - q_len + 1)) : k_len;
+    const int tiles = (hi + KT - 1) / KT, per = (tiles + c.splits - 1) / c.splits;
+    const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
+
+    const T *kp = (const T *)c.k + b * c.sk.batch + hk * c.sk.head;
+    const T *vp = (const T *)c.v + b * c.sv.batch + hk * c.sv.head;
+    const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
+
+    Frag q[NS], g[NS];
+    const int head = hk * c.group + pk.g;
+    const int64_t bh = (int64_t)b * c.kv_heads + hk;
+    float delta = 0.0f;
+    {
+        const T *rq = (const T *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + head * c.sq.head;
+        const T *rg = (const T *)c.d_o + b * c.s_do.batch + (int64_t)pk.q * c.s_do.row + head * c.s_do.head;
+        const T *ro = (const T *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + head * c.so.head;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            const uint4 z = make_uint4(0, 0, 0, 0);
+            q[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rq, 2 * t + half, c.d) : z);
+            g[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rg, 2 * t + half, c.d) : z);
+            const Frag o = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(ro, 2 * t + half, c.d) : z);
+#pragma unroll
+            for (int j = 0; j < M::kPiece; ++j) delta = fmaf((float)g[t][j], (float)o[j], delta);
+        }
+    }
+    delta = across_halves_sum(delta);
+    if (split == 0 && half == 0 && r < rows) c.delta[bh * rows + r] = delta;
+    RowStat st = {0.0f, INFINITY};
+    if (live) {
+        const float2 v = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
+        st = row_stat<kDiff>(v.x, v.y);
+    }
+    const float unit = kDiff ? kLog2eF : c.scale * kLog2eF;
+
+    uint4 kr[NPC], vr[NPC];
+    float br = 0.0f;
+    auto fetch = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            const int p = tid + i * NT, row = p / TL::kPieces, pc = p % TL::kPieces, key = tile * KT + row;
+            const bool there = key < k_len && (!BIAS || bp[key] != -INFINITY);
+            kr[i] = there ? load_piece<T, ALN>(kp + (int64_t)key * c.sk.row, pc, c.d) : make_uint4(0, 0, 0, 0);
+            vr[i] = there ? load_piece<T, ALN>(vp + (int64_t)key * c.sv.row, pc, c.d) : make_uint4(0, 0, 0, 0);
+        }
+        if (BIAS && tid < KT) br = tile * KT + tid < k_len ? bp[tile * KT + tid] : -INFINITY;
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
+            *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
+            *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
+        }
+        if (BIAS && tid < KT) lbias[buf][tid] = br;
+    };
+
+    f32x16 dq[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) dq[i] = (f32x16)(0.0f);
+    if (t0 < t1) {
+        fetch(t0);
+        put(0);
+    }
+    __syncthreads();
+    for (int tile = t0; tile < t1; ++tile) {
+        const int buf = (tile - t0) & 1;
+        const char *lk = lds + 2 * buf * kTile, *lv = lk + kTile;
+        if (tile + 1 < t1) fetch(tile + 1);
+        const bool masked = __any(limit < (tile + 1) * KT);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            f32x16 s = (f32x16)(0.0f), dp = (f32x16)(0.0f);
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                s = M::mma(TL::rows(lk, nb * 32, t, lane), q[t], s);
+                dp = M::mma(TL::rows(lv, nb * 32, t, lane), g[t], dp);
+            }
+            if constexpr (BIAS) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const f32x4 w = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * u + 4 * half];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], c.scale, w[j]);
+                }
+            }
+            if (masked) {
+                const int base = tile * KT + nb * 32 + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = base + 8 * (i / 4) + i % 4 < limit ? s[i] : -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                // (without bias m is taken off in the same fma that scales)
+                const float d = BIAS ? s[i] - st.m : kDiff ? fmaf(s[i], c.scale, -st.m) : s[i];
+                const float p = __builtin_amdgcn_exp2f(fmaf(d, unit, -st.off));
+                s[i] = p * (dp[i] - delta);
+            }
+#pragma unroll
+            for (int t = 0; t < NF; ++t) {
+                const Frag ds = M::pack(s, t);
+#pragma unroll
+                for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, nb * 32, t, i, lane), ds, dq[i]);
+            }
+        }
+        if (tile + 1 < t1) put(buf ^ 1);
+        __syncthreads();
+    }
+    if (r >= rows) return;
+    if (c.splits > 1) {
+        float *po = c.part + ((int64_t)split * c.batch * c.kv_heads * rows + bh * rows + r) * DP + 4 * half;
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                *(f32x4 *)(po + 32 * i + 8 * u) = f32x4{dq[i][4 * u], dq[i][4 * u + 1], dq[i][4 * u + 2], dq[i][4 * u + 3]};
+        return;
+    }
+    T *out = (T *)c.dq + b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + head * c.sdq.head;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) store_column<T, ALN>(out, dq[i], c.scale, 32 * i + 4 * half, c.d);
+}
+
+template <typename T, int DP, int RT, int WAVES, bool BIAS, bool ALN>
+__global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(const AttnCall c)
+{
+    using M = Mma<T>;
+    using Frag = typename M::Frag;
+    using TL = Tile<T, DP>;
+    constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = RT / 32, NF = 32 / M::kStep, ND = DP / 32;
+    constexpr int kTile = RT * TL::kRow, NPC = RT * TL::kPieces / NT;
+    constexpr bool kDiff = BIAS || sizeof(T) == 4;
+    static_assert(RT * TL::kPieces % NT == 0 && RT <= NT, "");
+    __shared__ __align__(16) char lds[4 * kTile];
+    __shared__ __align__(16) float lstat[2][3][RT];   // m, off, D
+    __shared__ __align__(16) int llimit[2][RT];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int rows = c.n * c.group, blocks = (c.m + 32 * WAVES - 1) / (32 * WAVES);
+    int id = xcd_order(blockIdx.x, gridDim.x);
+    const int split = id % c.splits;
+    id /= c.splits;
+    const int blk = id % blocks;   // (causal: the long ones first)
+    id /= blocks;
+    const int hk = id % c.kv_heads, b = id / c.kv_heads;
+    const int64_t bh = (int64_t)b * c.kv_heads + hk;
+
+    const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
+    const int q_len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
+    const int key0 = blk * 32 * WAVES, key = key0 + wave * 32 + (lane & 31);
+    const float bias = BIAS && key < k_len ? c.bias[b * c.bias_ld + key] : 0.0f;
+    const bool live = key < k_len && (!BIAS || bias != -INFINITY);
+    // rows that see a key of this block
+    const int first = c.causal ? min(q_len, max(0, key0 - (k_len - q_len))) : 0;
+    const int begin = first * c.group / RT, end = key0 < k_len ? (q_len * c.group + RT - 1) / RT : begin;
+    const int tiles = max(0, end - begin), per = (tiles + c.splits - 1) / c.splits;
+    const int t0 = begin + min(tiles, split * per), t1 = min(begin + tiles, t0 + per);
+
+    Frag k[NS], v[NS];
+    {
+        const T *rk = (const T *)c.k + b * c.sk.batch + (int64_t)key * c.sk.row + hk * c.sk.head;
+        const T *rv = (const T *)c.v + b * c.sv.batch + (int64_t)key * c.sv.row + hk * c.sv.head;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            const uint4 z = make_uint4(0, 0, 0, 0);
+            k[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rk, 2 * t + half, c.d) : z);
+            v[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rv, 2 * t + half, c.d) : z);
+        }
+    }
+    const float unit = kDiff ? kLog2eF : c.scale * kLog2eF;
+    const T *qp = (const T *)c.q + b * c.sq.batch + (int64_t)hk * c.group * c.sq.head;
+    const T *gp = (const T *)c.d_o + b * c.s_do.batch + (int64_t)hk * c.group * c.s_do.head;
+
+    uint4 qr[NPC], gr[NPC];
+    RowStat st = {0.0f, INFINITY};
+    float delta = 0.0f;
+    int limit = 0;
+    auto fetch = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            const int p = tid + i * NT, row = tile * RT + p / TL::kPieces, pc = p % TL::kPieces;
+            const Packed pk = unpack(row, c.group);
+            const bool there = pk.q < q_len;
+            qr[i] = there ? load_piece<T, ALN>(qp + (int64_t)pk.q * c.sq.row + pk.g * c.sq.head, pc, c.d) : make_uint4(0, 0, 0, 0);
+            gr[i] = there ? load_piece<T, ALN>(gp + (int64_t)pk.q * c.s_do.row + pk.g * c.s_do.head, pc, c.d) : make_uint4(0, 0, 0, 0);
+        }
+        if (tid < RT) {
+            const Packed pk = unpack(tile * RT + tid, c.group);
+            st = {0.0f, INFINITY};
+            delta = 0.0f;
+            limit = 0;
+            if (pk.q < q_len) {
+                const float2 w = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
+                st = row_stat<kDiff>(w.x, w.y);
+                delta = c.delta[bh * rows + tile * RT + tid];
+                limit = c.causal ? pk.q + k_len - q_len + 1 : c.m;
+            }
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
+            *(uint4 *)(lds + (2 * buf) * kTile + at) = qr[i];
+            *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = gr[i];
+        }
+        if (tid < RT) {
+            lstat[buf][0][tid] = st.m;
+            lstat[buf][1][tid] = st.off;
+            lstat[buf][2][tid] = delta;
+            llimit[buf][tid] = limit;
+        }
+    };
+
+    f32x16 dk[ND], dv[ND];
+    float db = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) dk[i] = dv[i] = (f32x16)(0.0f);
+    if (t0 < t1) {
+        fetch(t0);
+        put(0);
+    }
+    __syncthreads();
+    for (int tile = t0; tile < t1; ++tile) {
+        const int buf = (tile - t0) & 1;
+        const char *lq = lds + 2 * buf * kTile, *lg = lq + kTile;
+        if (tile + 1 < t1) fetch(tile + 1);
+        // the tile's first row sees fewer keys than the others
+        const bool masked = c.causal && tile * RT / c.group + k_len - q_len + 1 < key0 + 32 * WAVES;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            f32x16 s = (f32x16)(0.0f), dp = (f32x16)(0.0f);
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                s = M::mma(TL::rows(lq, nb * 32, t, lane), k[t], s);
+                dp = M::mma(TL::rows(lg, nb * 32, t, lane), v[t], dp);
+            }
+            f32x16 p;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = nb * 32 + 8 * u + 4 * half;
+                const f32x4 off = *(const f32x4 *)&lstat[buf][1][at], dl = *(const f32x4 *)&lstat[buf][2][at];
+                f32x4 m;
+                if (kDiff) m = *(const f32x4 *)&lstat[buf][0][at];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 4 * u + j;
+                    const float d = BIAS ? fmaf(s[i], c.scale, bias) - m[j] : kDiff ? fmaf(s[i], c.scale, -m[j]) : s[i];
+                    float e = __builtin_amdgcn_exp2f(fmaf(d, unit, -off[j]));
+                    if (masked && key >= llimit[buf][at + j]) e = 0.0f;
+                    p[i] = e;
+                    s[i] = e * (dp[i] - dl[j]);
+                    if (BIAS) db += s[i];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < NF; ++t) {
+                const Frag pf = M::pack(p, t), sf = M::pack(s, t);
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    dv[i] = M::mma(TL::cols(lg, nb * 32, t, i, lane), pf, dv[i]);
+                    dk[i] = M::mma(TL::cols(lq, nb * 32, t, i, lane), sf, dk[i]);
+                }
+            }
+        }
+        if (tile + 1 < t1) put(buf ^ 1);
+        __syncthreads();
+    }
+    if (BIAS) db = across_halves_sum(db);
+    if (key >= c.m) return;
+    if (!live) {   // (what its column computed came from zeros, and may be anything)
+#pragma unroll
+        for (int i = 0; i < ND; ++i) dk[i] = dv[i] = (f32x16)(0.0f);
+        db = 0.0f;
+    }
+    const int64_t slot = ((int64_t)split * c.batch * c.kv_heads + bh) * c.m + key;
+    if (BIAS && c.dbias && half == 0) c.dbias_part[slot] = db;
+    if (c.splits > 1) {
+        float *po = c.part + slot * 2 * DP + 4 * half;
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                *(f32x4 *)(po + 32 * i + 8 * u) = f32x4{dk[i][4 * u], dk[i][4 * u + 1], dk[i][4 * u + 2], dk[i][4 * u + 3]};
+                *(f32x4 *)(po + DP + 32 * i + 8 * u) = f32x4{dv[i][4 * u], dv[i][4 * u + 1], dv[i][4 * u + 2], dv[i][4 * u + 3]};
+            }
+        return;
+    }
+    T *ok = (T *)c.dk + b * c.sdk.batch + (int64_t)key * c.sdk.row + hk * c.sdk.head;
+    T *ov = (T *)c.dv + b * c.sdv.batch + (int64_t)key * c.sdv.row + hk * c.sdv.head;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) {
+        store_column<T, ALN>(ok, dk[i], c.scale, 32 * i + 4 * half, c.d);
+        store_column<T, ALN>(ov, dv[i], 1.0f, 32 * i + 4 * half, c.d);
+    }
+}
+
+// Sums over the splits: a wave takes a row of dq (KV: of dk and dv), in the order of the splits.
+template <typename T, int DP, bool KV>
+__global__ __launch_bounds__(256) void k_attn_grad_join(const AttnCall c)
+{
+    const int lane = threadIdx.x & 63, rows = KV ? c.m : c.n * c.group;
+    const int64_t total = (int64_t)c.batch * c.kv_heads * rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= total) return;
+    constexpr int W = KV ? 2 * DP : DP;
+    const int64_t bh = at / rows;
+    const int hk = (int)(bh % c.kv_heads), b = (int)(bh / c.kv_heads), r = (int)(at - bh * rows);
+    for (int col = lane; col < W; col += 64) {
+        float acc = 0.0f;
+        for (int s = 0; s < c.splits; ++s) acc += c.part[(s * total + at) * W + col];
+        const int e = col % DP;
+        if (e >= c.d) continue;
+        if constexpr (KV) {
+            if (col < DP) ((T *)c.dk)[b * c.sdk.batch + (int64_t)r * c.sdk.row + hk * c.sdk.head + e] = (T)(acc * c.scale);
+            else ((T *)c.dv)[b * c.sdv.batch + (int64_t)r * c.sdv.row + hk * c.sdv.head + e] = (T)acc;
+        } else {
+            const Packed pk = unpack(r, c.group);
+            ((T *)c.dq)[b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + (hk * c.group + pk.g) * c.sdq.head + e] = (T)(acc * c.scale);
+        }
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void k_attn_dbias(const AttnCall c)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (int64_t)c.batch * c.m) return;
+    const int64_t b = at / c.m, key = at - b * c.m;
+    float acc = 0.0f;
+    for (int s = 0; s < c.splits; ++s)
+        for (int h = 0; h < c.kv_heads; ++h) acc += c.dbias_part[(((int64_t)s * c.batch + b) * c.kv_heads + h) * c.m + key];
+    ((T *)c.dbias)[b * c.dbias_ld + key] = (T)acc;
+}
+
+template <typename T, int DP>
+fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool aligned)
+{
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32, RT = sizeof(T) == 2 && DP < 128 ? 64 : 32;
+    Arena A;
+    a.delta = (float *)(ws + A.take(p.delta_bytes));
+    float *dq_part = (float *)(ws + A.take(p.dq_bytes)), *dkv_part = (float *)(ws + A.take(p.dkv_bytes));
+    a.dbias_part = (float *)(ws + A.take(p.dbias_bytes));
+    const int64_t heads = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.n * a.group;
+    a.splits = p.q_splits;
+    a.part = dq_part;
+    if (p.q_grid) {
+        const unsigned grid = (unsigned)p.q_grid;
+        if (a.bias) {
+            if (aligned) k_attn_dq<T, DP, KT, 4, true, true><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dq<T, DP, KT, 4, true, false><<<grid, 256, 0, c->stream>>>(a);
+        } else {
+            if (aligned) k_attn_dq<T, DP, KT, 4, false, true><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dq<T, DP, KT, 4, false, false><<<grid, 256, 0, c->stream>>>(a);
+        }
+        if (a.splits > 1) k_attn_grad_join<T, DP, false><<<(unsigned)ceil_div(heads * rows, 4), 256, 0, c->stream>>>(a);
+    }
+    a.splits = p.k_splits;
+    a.part = dkv_part;
+    if (p.k_grid) {
+        const unsigned grid = (unsigned)p.k_grid;
+        if (a.bias) {
+            if (aligned) k_attn_dkv<T, DP, RT, 4, true, true><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dkv<T, DP, RT, 4, true, false><<<grid, 256, 0, c->stream>>>(a);
+        } else {
+            if (aligned) k_attn_dkv<T, DP, RT, 4, false, true><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dkv<T, DP, RT, 4, false, false><<<grid, 256, 0, c->stream>>>(a);
+        }
+        if (a.splits > 1) k_attn_grad_join<T, DP, true><<<(unsigned)ceil_div(heads * a.m, 4), 256, 0, c->stream>>>(a);
+        if (a.dbias) k_attn_dbias<T><<<(unsigned)ceil_div((int64_t)a.batch * a.m, 256), 256, 0, c->stream>>>(a);
+    }
+    FS_HIP(c, hipGetLastError());
+    return FS_OK;
+}
+
+template <typename T> fs_status by_width(Ctx *c, const AttnCall &a, const AttnGradPlan &p, char *ws, bool aligned)
+{
+    switch ((a.d + 31) / 32) {
+    case 1: return run<T, 32>(c, a, p, ws, aligned);
+    case 2: return run<T, 64>(c, a, p, ws, aligned);
+    case 3: return run<T, 96>(c, a, p, ws, aligned);
+    default: return run<T, 128>(c, a, p, ws, aligned);
+    }
+}
+
+}  // namespace
+
+AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
+{
+    AttnGradPlan p;
+    const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads, dp = round_up(a.d, 32);
+    const int64_t want = 2 * (int64_t)c->num_cu;
+    const int64_t qb = ceil_div(rows, 128) * heads, kb = ceil_div(a.m, 128) * heads;
+    const int64_t kt = ceil_div(a.m, f32 ? 32 : 64), rt = ceil_div(rows, 32);
+    p.q_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(qb, 1), kt / 4));
+    p.k_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(kb, 1), rt / 8));
+    p.q_grid = qb * p.q_splits;
+    p.k_grid = kb * p.k_splits;
+    p.delta_bytes = (size_t)(heads * rows) * 4;
+    p.dq_bytes = p.q_splits > 1 ? (size_t)(heads * rows * dp * p.q_splits) * 4 : 0;
+    p.dkv_bytes = p.k_splits > 1 ? (size_t)(heads * a.m * dp * 2 * p.k_splits) * 4 : 0;
+    p.dbias_bytes = a.dbias ? (size_t)(heads * a.m * p.k_splits) * 4 : 0;
+    return p;
+}
+
+fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool f32, bool aligned)
+{
+    return f32 ? by_width<float>(c, a, p, ws, aligned) : by_width<__bf16>(c, a, p, ws, aligned);
+}
+
+}  // namespace fs

@@ -688,4 +688,13 @@ fs_status bf16_apply(Ctx *c, const Prepared *P, const Side *res, const Side *str
 void prof_begin(Ctx *c, double pairs, int kind = 0);
 void prof_end(Ctx *c);
 
+// layer norm (fs_norm.hip); part: [norm_grad_blocks][2][cols] floats where a weight's gradient is wanted
+int norm_grad_blocks(const Ctx *c, int64_t rows);
+fs_status launch_norm(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, const void *beta,
+                      int32_t wtype, float eps, void *y, int64_t ldy, float *stat);
+fs_status launch_norm_grad(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, int32_t wtype,
+                           const float *stat, const void *dy, int64_t lddy, void *dx, int64_t lddx, float *dgamma, float *dbeta, float *part);
+// AdamW over many tensors (fs_adamw.hip)
+fs_status launch_adamw(Ctx *c, const fs_adamw_args *a, const fs_adamw_tensor *t, int32_t count, bool master);
+
 }  // namespace fs
