@@ -1488,7 +1488,7 @@ fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o,
     const bool f32 = attn->dtype == FS_F32;
     const AttnGradPlan p = attn_grad_plan(c, a, f32);
     Arena A;
-    A.take(p.delta_bytes);
+    A.take(p.stat_bytes);
     A.take(p.dq_bytes);
     A.take(p.dkv_bytes);
     A.take(p.dbias_bytes);

@@ -58,42 +58,89 @@ template <> struct Mma<float> {
 
 // A tile of rows in LDS, DP elements each (zero beyond d).  16-byte pieces are permuted within their row so that the lanes of a
 // fragment read, which take one piece each of 32 consecutive rows, meet in as few banks as there are.
+using LdsPtr = const __attribute__((address_space(3))) char *;
 template <typename T, int DP> struct Tile {
     static constexpr int kRow = DP * (int)sizeof(T);   // bytes
     static constexpr int kPieces = kRow / 16;
-    static __device__ inline int swz(int row) { return kPieces % 8 == 0 ? row & 7 : (row >> 1) & 3; }
+    static constexpr bool kWide = kPieces % 8 == 0;
+    static __device__ inline int swz(int row) { return kWide ? row & 7 : (row >> 1) & 3; }
     static __device__ inline int at(int row, int piece) { return row * kRow + ((piece ^ swz(row)) << 4); }
-    // operand with the tile's rows as rows: step t of the contraction over coordinates
-    static __device__ inline typename Mma<T>::Frag rows(const char *lds, int row0, int t, int lane)
+
+    // The permutation touches the lowest two or three bits of a piece's number: fragments that differ in higher bits, and in their
+    // first row (a multiple of 32 or of a step), are at constant distances.  What is left for a lane to compute once:
+    static constexpr int kRowBases = kWide ? 4 : 2, kColBases = kWide ? 2 : 1;
+    struct Lanes {
+        int row[kRowBases], col[kColBases];
+    };
+    static __device__ inline Lanes lanes(int lane)
     {
-        return *(const typename Mma<T>::Frag *)(lds + at(row0 + (lane & 31), 2 * t + (lane >> 5)));
+        Lanes b;
+#pragma unroll
+        for (int t = 0; t < kRowBases; ++t) b.row[t] = at(lane & 31, 2 * t + (lane >> 5));
+        const int i = lane & 15;
+#pragma unroll
+        for (int q = 0; q < kColBases; ++q) {
+            if constexpr (sizeof(T) == 2)
+                b.col[q] = at(4 * (lane >> 5) + (i >> 2), 4 * q + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) + (i & 1) * 8;
+            else
+                b.col[q] = 0;
+        }
+        return b;
+    }
+    // operand with the tile's rows as rows: step t of the contraction over coordinates
+    static __device__ inline typename Mma<T>::Frag rows(LdsPtr lds, const Lanes &b, int row0, int t)
+    {
+        return *(const __attribute__((address_space(3))) typename Mma<T>::Frag *)(lds + b.row[t % kRowBases] + row0 * kRow +
+                                                                                  t / kRowBases * kRowBases * 32);
     }
     // operand with coordinates 32 db .. 32 db + 31 as rows: step t of the contraction over the 32 rows from row0 on, in the order
     // in which a product's registers hold them
-    static __device__ inline typename Mma<T>::Frag cols(const char *lds, int row0, int t, int db, int lane)
+    static __device__ inline typename Mma<T>::Frag cols(LdsPtr lds, const Lanes &b, int row0, int t, int db, int lane)
     {
         if constexpr (sizeof(T) == 2) {
             // sixteen lanes read 4 rows x 16 coordinates, eight bytes each, and get a coordinate each: its four rows
-            const int i = lane & 15, piece = 4 * db + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
-            const int r = row0 + 16 * t + 4 * (lane >> 5) + (i >> 2);
             using P = __attribute__((address_space(3))) s16x4 *;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds_offset(lds) + at(r, piece) + (i & 1) * 8));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds_offset(lds) + at(r + 8, piece) + (i & 1) * 8));
+            const LdsPtr at = lds + b.col[db % kColBases] + (row0 + 16 * t) * kRow + db / kColBases * kColBases * 64;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(at + 8 * kRow));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             f32x4 f;
             const int c = 32 * db + (lane & 31);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                f[j] = *(const float *)(lds + at(row0 + 8 * t + 4 * (lane >> 5) + j, c >> 2) + (c & 3) * 4);
+                f[j] = *(const __attribute__((address_space(3))) float *)(lds + at(row0 + 8 * t + 4 * (lane >> 5) + j, c >> 2) + (c & 3) * 4);
             return f;
         }
     }
-    static __device__ inline unsigned lds_offset(const char *p)
+};
+__device__ inline unsigned lds_address(LdsPtr p) { return (unsigned)(uintptr_t)p; }
+
+// How a tile comes to LDS.
+//  kDma   straight from memory (direct loads, 16 bytes a lane, no registers): aligned rows whose offsets within a tile fit
+//         32 bits, no bias
+//  kVec   through registers, 16 bytes a load: aligned rows
+//  kAny   through registers, an element a load
+// The registers' way can leave out what removed keys (bias of minus infinity) hold; the direct one reads whole tiles.
+enum Load { kDma, kVec, kAny };
+
+// Direct loads of a tile of ROWS rows by NT threads: LDS takes consecutive 16-byte pieces of consecutive lanes, so a lane fetches the piece
+// that the permutation puts there.  Pieces beyond d are left alone (zeroed once).
+template <typename T, int DP, int ROWS, int NT> struct Dma {
+    using TL = Tile<T, DP>;
+    static constexpr int kCount = ROWS * TL::kPieces / NT, kTile = ROWS * TL::kRow;
+    static __device__ inline int row(int tid, int i) { return (tid + i * NT) / TL::kPieces; }
+    static __device__ inline int piece(int tid, int i) { return ((tid + i * NT) % TL::kPieces) ^ TL::swz(row(tid, i)); }
+    // base: of the tile's first row (uniform); off[i]: bytes from there; lds: of the tile (uniform)
+    static __device__ inline void load(const char *base, const unsigned (&off)[kCount], unsigned lds, int tid, int d)
     {
-        return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds + (tid >> 6) * 1024);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i)
+            if (d == DP || piece(tid, i) * Mma<T>::kPiece < d) dma16s(base, off[i], to + i * NT * 16);
     }
 };
+__device__ inline void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // 16 bytes of a row: elements piece * kPiece .. of d, zero beyond.  ALN: rows are 16-byte aligned and d is a multiple of kPiece.
 template <typename T, bool ALN> __device__ inline uint4 load_piece(const T *row, int piece, int d)
@@ -151,7 +198,7 @@ struct AttnCall {
     void *dq, *dk, *dv, *dbias;
     HeadsAt sdq, sdk, sdv;
     int64_t dbias_ld;
-    float *delta;                // backward: [batch][kv head][packed row] <do, o>
+    float *row_stat;             // backward: [batch][kv head][3][packed rows, padded]: see k_attn_dq
     const int32_t *q_len, *k_len;
     const float *bias;
     int64_t bias_ld;
@@ -194,7 +241,7 @@ fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bo
 struct AttnGradPlan {
     int q_splits, k_splits;
     int64_t q_grid, k_grid;
-    size_t delta_bytes, dq_bytes, dkv_bytes, dbias_bytes;
+    size_t stat_bytes, dq_bytes, dkv_bytes, dbias_bytes;
 };
 AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32);
 // `ws`: the bytes of the plan, each piece rounded up to 256

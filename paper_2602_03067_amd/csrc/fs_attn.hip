@@ -15,14 +15,19 @@ constexpr float kLog2eF = 1.44269504088896340736f;
 // relative rounding at any size.
 constexpr float kSlack = 8.0f;
 
-template <typename T, int DP, int KT, int WAVES, bool BIAS, bool ALN>
-__global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
+// waves per SIMD: what registers allow without spills
+constexpr int min_waves(size_t elem, int dp) { return elem == 4 && dp >= 96 ? 1 : 2; }
+
+template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD>
+__global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(const AttnCall c)
 {
     using M = Mma<T>;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
+    using D = Dma<T, DP, KT, 64 * WAVES>;
+    constexpr bool ALN = LOAD != kAny;
     constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
-    constexpr int kTile = KT * TL::kRow, NPC = KT * TL::kPieces / NT;
+    constexpr int kTile = D::kTile, NPC = D::kCount;
     static_assert(KT * TL::kPieces % NT == 0, "");
     __shared__ __align__(16) char lds[4 * kTile];
     __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
@@ -51,7 +56,66 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
     const T *kp = (const T *)c.k + b * c.sk.batch + hk * c.sk.head;
     const T *vp = (const T *)c.v + b * c.sv.batch + hk * c.sv.head;
     const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
+    const LdsPtr base = (LdsPtr)lds;
 
+    // what a thread fetches of a tile
+    unsigned ko[LOAD == kDma ? NPC : 1], vo[LOAD == kDma ? NPC : 1];
+    uint4 kr[LOAD == kDma ? 1 : NPC], vr[LOAD == kDma ? 1 : NPC];
+    float br = 0.0f;
+    if constexpr (LOAD == kDma) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+            vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+        }
+        if (c.d != DP && t0 < t1) {   // pieces that no load writes
+            for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+        }
+    }
+    // kDma: the whole way; otherwise to registers
+    auto fetch = [&](int tile, int buf) {
+        if constexpr (LOAD == kDma) {
+            const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
+            const unsigned to = lds_address(base) + 2 * buf * kTile;
+            if ((tile + 1) * KT <= k_len) {
+                D::load(kb, ko, to, tid, c.d);
+                D::load(vb, vo, to + kTile, tid, c.d);
+            } else {   // the last row again beyond the end
+                unsigned ke[NPC], ve[NPC];
+#pragma unroll
+                for (int i = 0; i < NPC; ++i) {
+                    const int row = min(D::row(tid, i), k_len - 1 - tile * KT);
+                    ke[i] = (unsigned)(row * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+                    ve[i] = (unsigned)(row * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+                }
+                D::load(kb, ke, to, tid, c.d);
+                D::load(vb, ve, to + kTile, tid, c.d);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) {
+                const int p = tid + i * NT, pc = p % TL::kPieces, key = tile * KT + p / TL::kPieces, at = min(key, k_len - 1);
+                kr[i] = load_piece<T, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
+                vr[i] = load_piece<T, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
+                if (BIAS && bp[at] == -INFINITY) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);   // what removed keys hold does not matter
+            }
+            if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
+        }
+    };
+    auto put = [&](int buf) {
+        if constexpr (LOAD != kDma) {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) {
+                const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
+                *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
+                *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
+            }
+            if (BIAS && tid < KT) lbias[buf][tid] = br;
+        }
+    };
+
+    if (t0 < t1) fetch(t0, 0);
     Frag q[NS];
     {
         const T *row = (const T *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + (hk * c.group + pk.g) * c.sq.head;
@@ -59,29 +123,6 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
         for (int t = 0; t < NS; ++t)
             q[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(row, 2 * t + half, c.d) : make_uint4(0, 0, 0, 0));
     }
-
-    uint4 kr[NPC], vr[NPC];
-    float br = 0.0f;
-    auto fetch = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < NPC; ++i) {
-            const int p = tid + i * NT, row = p / TL::kPieces, pc = p % TL::kPieces, key = tile * KT + row;
-            const bool there = key < k_len && (!BIAS || bp[key] != -INFINITY);   // what removed keys hold does not matter
-            kr[i] = there ? load_piece<T, ALN>(kp + (int64_t)key * c.sk.row, pc, c.d) : make_uint4(0, 0, 0, 0);
-            vr[i] = there ? load_piece<T, ALN>(vp + (int64_t)key * c.sv.row, pc, c.d) : make_uint4(0, 0, 0, 0);
-        }
-        if (BIAS && tid < KT) br = tile * KT + tid < k_len ? bp[tile * KT + tid] : -INFINITY;
-    };
-    auto put = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < NPC; ++i) {
-            const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
-            *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
-            *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
-        }
-        if (BIAS && tid < KT) lbias[buf][tid] = br;
-    };
-
     f32x16 o[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) o[i] = (f32x16)(0.0f);
@@ -91,23 +132,23 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
     // precision is not to lose an ulp of the larger of the two.  In bf16 without bias one fma does.
     constexpr bool kDiff = BIAS || sizeof(T) == 4;
     float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
+    const typename TL::Lanes ln = TL::lanes(lane);
 
-    if (t0 < t1) {
-        fetch(t0);
-        put(0);
-    }
+    if (t0 < t1) put(0);
+    dma_wait();   // (of q as well: not inside the loop, where it would wait for the next tile)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
     for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
-        const char *lk = lds + 2 * buf * kTile, *lv = lk + kTile;
-        if (tile + 1 < t1) fetch(tile + 1);
+        const LdsPtr lk = base + 2 * buf * kTile, lv = lk + kTile;
+        if (tile + 1 < t1) fetch(tile + 1, buf ^ 1);
 
         f32x16 s[NB];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             s[nb] = (f32x16)(0.0f);
 #pragma unroll
-            for (int t = 0; t < NS; ++t) s[nb] = M::mma(TL::rows(lk, nb * 32, t, lane), q[t], s[nb]);
+            for (int t = 0; t < NS; ++t) s[nb] = M::mma(TL::rows(lk, ln, nb * 32, t), q[t], s[nb]);
         }
         if constexpr (BIAS) {
 #pragma unroll
@@ -119,8 +160,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
                     for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], c.scale, w[j]);
                 }
         }
-        const int base = tile * KT + 4 * half;
         if (__any(limit < (tile + 1) * KT)) {
+            const int base = tile * KT + 4 * half;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -160,9 +201,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn(const AttnCall c)
             for (int t = 0; t < NF; ++t) {
                 const Frag p = M::pack(s[nb], t);
 #pragma unroll
-                for (int i = 0; i < ND; ++i) o[i] = M::mma(TL::cols(lv, nb * 32, t, i, lane), p, o[i]);
+                for (int i = 0; i < ND; ++i) o[i] = M::mma(TL::cols(lv, ln, nb * 32, t, i, lane), p, o[i]);
             }
-        if (tile + 1 < t1) put(buf ^ 1);
+        if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
+        if (LOAD == kDma) dma_wait();
         __syncthreads();
     }
 
@@ -224,14 +266,16 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnCall c)
 }
 
 template <typename T, int DP, int KT, int WAVES>
-fs_status run(Ctx *c, const AttnCall &a, bool aligned, int64_t grid)
+fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
 {
+    const unsigned g = (unsigned)grid, nt = 64 * WAVES;
     if (a.bias) {
-        if (aligned) k_attn<T, DP, KT, WAVES, true, true><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
-        else k_attn<T, DP, KT, WAVES, true, false><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
+        if (load != kAny) k_attn<T, DP, KT, WAVES, true, kVec><<<g, nt, 0, c->stream>>>(a);
+        else k_attn<T, DP, KT, WAVES, true, kAny><<<g, nt, 0, c->stream>>>(a);
     } else {
-        if (aligned) k_attn<T, DP, KT, WAVES, false, true><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
-        else k_attn<T, DP, KT, WAVES, false, false><<<(unsigned)grid, 64 * WAVES, 0, c->stream>>>(a);
+        if (load == kDma) k_attn<T, DP, KT, WAVES, false, kDma><<<g, nt, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn<T, DP, KT, WAVES, false, kVec><<<g, nt, 0, c->stream>>>(a);
+        else k_attn<T, DP, KT, WAVES, false, kAny><<<g, nt, 0, c->stream>>>(a);
     }
     if (a.splits > 1) {
         const int64_t total = (int64_t)a.batch * a.kv_heads * a.n * a.group;
@@ -242,23 +286,23 @@ fs_status run(Ctx *c, const AttnCall &a, bool aligned, int64_t grid)
 }
 
 template <typename T>
-fs_status by_width(Ctx *c, const AttnCall &a, bool aligned, int waves, int64_t grid)
+fs_status by_width(Ctx *c, const AttnCall &a, Load load, int waves, int64_t grid)
 {
     constexpr int KT = sizeof(T) == 2 ? 64 : 32;
     const int dp = (a.d + 31) / 32;
     if (waves == 1) {
         switch (dp) {
-        case 1: return run<T, 32, 32, 1>(c, a, aligned, grid);
-        case 2: return run<T, 64, 32, 1>(c, a, aligned, grid);
-        case 3: return run<T, 96, 32, 1>(c, a, aligned, grid);
-        default: return run<T, 128, 32, 1>(c, a, aligned, grid);
+        case 1: return run<T, 32, 32, 1>(c, a, load, grid);
+        case 2: return run<T, 64, 32, 1>(c, a, load, grid);
+        case 3: return run<T, 96, 32, 1>(c, a, load, grid);
+        default: return run<T, 128, 32, 1>(c, a, load, grid);
         }
     }
     switch (dp) {
-    case 1: return run<T, 32, KT, 4>(c, a, aligned, grid);
-    case 2: return run<T, 64, KT, 4>(c, a, aligned, grid);
-    case 3: return run<T, 96, KT, 4>(c, a, aligned, grid);
-    default: return run<T, 128, KT, 4>(c, a, aligned, grid);
+    case 1: return run<T, 32, KT, 4>(c, a, load, grid);
+    case 2: return run<T, 64, KT, 4>(c, a, load, grid);
+    case 3: return run<T, 96, KT, 4>(c, a, load, grid);
+    default: return run<T, 128, KT, 4>(c, a, load, grid);
     }
 }
 
@@ -282,7 +326,10 @@ AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
 
 fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bool aligned)
 {
-    return f32 ? by_width<float>(c, a, aligned, p.waves, p.grid) : by_width<__bf16>(c, a, aligned, p.waves, p.grid);
+    // (offsets of 64 rows in 32 bits)
+    const int64_t most = std::max(a.sk.row, a.sv.row) * (f32 ? 4 : 2) * 64;
+    const Load load = !aligned ? kAny : most < (int64_t(1) << 31) ? kDma : kVec;
+    return f32 ? by_width<float>(c, a, load, p.waves, p.grid) : by_width<__bf16>(c, a, load, p.waves, p.grid);
 }
 
 }  // namespace fs

@@ -25,16 +25,26 @@ template <bool DIFF> __device__ inline RowStat row_stat(float top, float sum)
     return DIFF ? RowStat{top, lg} : RowStat{0.0f, fmaf(top, kLog2eF, lg)};
 }
 
-template <typename T, int DP, int KT, int WAVES, bool BIAS, bool ALN>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
+constexpr int kRowBlock = 128;   // packed rows of a dq workgroup; the row statistics are padded to whole ones
+__device__ inline int64_t round_up_rows(int rows) { return ((int64_t)rows + kRowBlock - 1) / kRowBlock * kRowBlock; }
+constexpr int row_tile(size_t elem) { return elem == 2 ? 64 : 32; }
+
+// waves per SIMD: what registers allow without spills
+constexpr int dq_waves(size_t elem, int dp) { return elem == 4 && dp >= 96 ? 1 : 2; }
+constexpr int dkv_waves(size_t elem, int dp) { return elem == 4 ? (dp >= 64 ? 1 : 2) : dp >= 160 ? 1 : 2; }
+
+template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD>
+__global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq(const AttnCall c)
 {
     using M = Mma<T>;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
+    using D = Dma<T, DP, KT, 64 * WAVES>;
+    constexpr bool ALN = LOAD != kAny;
     constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
-    constexpr int kTile = KT * TL::kRow, NPC = KT * TL::kPieces / NT;
+    constexpr int kTile = D::kTile, NPC = D::kCount;
     constexpr bool kDiff = BIAS || sizeof(T) == 4;
-    static_assert(KT * TL::kPieces % NT == 0, "");
+    static_assert(KT * TL::kPieces % NT == 0 && 32 * WAVES == kRowBlock, "");
     __shared__ __align__(16) char lds[4 * kTile];
     __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
 
@@ -43,7 +53,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
     int id = xcd_order(blockIdx.x, gridDim.x);
     const int split = id % c.splits;
     id /= c.splits;
-    const int blk = blocks - 1 - id % blocks;
+    const int blk = blocks - 1 - id % blocks;   // (causal: the long ones first)
     id /= blocks;
     const int hk = id % c.kv_heads, b = id / c.kv_heads;
 
@@ -61,7 +71,65 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
     const T *kp = (const T *)c.k + b * c.sk.batch + hk * c.sk.head;
     const T *vp = (const T *)c.v + b * c.sv.batch + hk * c.sv.head;
     const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
+    const LdsPtr base = (LdsPtr)lds;
 
+    // (tiles of keys as in k_attn)
+    unsigned ko[LOAD == kDma ? NPC : 1], vo[LOAD == kDma ? NPC : 1];
+    uint4 kr[LOAD == kDma ? 1 : NPC], vr[LOAD == kDma ? 1 : NPC];
+    float br = 0.0f;
+    if constexpr (LOAD == kDma) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+            vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+        }
+        if (c.d != DP && t0 < t1) {
+            for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+        }
+    }
+    auto fetch = [&](int tile, int buf) {
+        if constexpr (LOAD == kDma) {
+            const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
+            const unsigned to = lds_address(base) + 2 * buf * kTile;
+            if ((tile + 1) * KT <= k_len) {
+                D::load(kb, ko, to, tid, c.d);
+                D::load(vb, vo, to + kTile, tid, c.d);
+            } else {
+                unsigned ke[NPC], ve[NPC];
+#pragma unroll
+                for (int i = 0; i < NPC; ++i) {
+                    const int row = min(D::row(tid, i), k_len - 1 - tile * KT);
+                    ke[i] = (unsigned)(row * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+                    ve[i] = (unsigned)(row * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+                }
+                D::load(kb, ke, to, tid, c.d);
+                D::load(vb, ve, to + kTile, tid, c.d);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) {
+                const int p = tid + i * NT, pc = p % TL::kPieces, key = tile * KT + p / TL::kPieces, at = min(key, k_len - 1);
+                kr[i] = load_piece<T, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
+                vr[i] = load_piece<T, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
+                if (BIAS && bp[at] == -INFINITY) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+            }
+            if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
+        }
+    };
+    auto put = [&](int buf) {
+        if constexpr (LOAD != kDma) {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) {
+                const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
+                *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
+                *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
+            }
+            if (BIAS && tid < KT) lbias[buf][tid] = br;
+        }
+    };
+
+    if (t0 < t1) fetch(t0, 0);
     Frag q[NS], g[NS];
     const int head = hk * c.group + pk.g;
     const int64_t bh = (int64_t)b * c.kv_heads + hk;
@@ -81,56 +149,40 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
         }
     }
     delta = across_halves_sum(delta);
-    if (split == 0 && half == 0 && r < rows) c.delta[bh * rows + r] = delta;
     RowStat st = {0.0f, INFINITY};
     if (live) {
         const float2 v = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
         st = row_stat<kDiff>(v.x, v.y);
     }
+    if (split == 0 && half == 0) {   // for the other pass, whole blocks of rows
+        const int64_t pad = (int64_t)blocks * 32 * WAVES;
+        float *out = c.row_stat + 3 * bh * pad + r;
+        out[0] = st.off;
+        out[pad] = delta;
+        if (kDiff) out[2 * pad] = st.m;
+    }
     const float unit = kDiff ? kLog2eF : c.scale * kLog2eF;
-
-    uint4 kr[NPC], vr[NPC];
-    float br = 0.0f;
-    auto fetch = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < NPC; ++i) {
-            const int p = tid + i * NT, row = p / TL::kPieces, pc = p % TL::kPieces, key = tile * KT + row;
-            const bool there = key < k_len && (!BIAS || bp[key] != -INFINITY);
-            kr[i] = there ? load_piece<T, ALN>(kp + (int64_t)key * c.sk.row, pc, c.d) : make_uint4(0, 0, 0, 0);
-            vr[i] = there ? load_piece<T, ALN>(vp + (int64_t)key * c.sv.row, pc, c.d) : make_uint4(0, 0, 0, 0);
-        }
-        if (BIAS && tid < KT) br = tile * KT + tid < k_len ? bp[tile * KT + tid] : -INFINITY;
-    };
-    auto put = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < NPC; ++i) {
-            const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
-            *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
-            *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
-        }
-        if (BIAS && tid < KT) lbias[buf][tid] = br;
-    };
+    const typename TL::Lanes ln = TL::lanes(lane);
 
     f32x16 dq[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) dq[i] = (f32x16)(0.0f);
-    if (t0 < t1) {
-        fetch(t0);
-        put(0);
-    }
+    if (t0 < t1) put(0);
+    dma_wait();
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
     for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
-        const char *lk = lds + 2 * buf * kTile, *lv = lk + kTile;
-        if (tile + 1 < t1) fetch(tile + 1);
+        const LdsPtr lk = base + 2 * buf * kTile, lv = lk + kTile;
+        if (tile + 1 < t1) fetch(tile + 1, buf ^ 1);
         const bool masked = __any(limit < (tile + 1) * KT);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             f32x16 s = (f32x16)(0.0f), dp = (f32x16)(0.0f);
 #pragma unroll
             for (int t = 0; t < NS; ++t) {
-                s = M::mma(TL::rows(lk, nb * 32, t, lane), q[t], s);
-                dp = M::mma(TL::rows(lv, nb * 32, t, lane), g[t], dp);
+                s = M::mma(TL::rows(lk, ln, nb * 32, t), q[t], s);
+                dp = M::mma(TL::rows(lv, ln, nb * 32, t), g[t], dp);
             }
             if constexpr (BIAS) {
 #pragma unroll
@@ -156,10 +208,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
             for (int t = 0; t < NF; ++t) {
                 const Frag ds = M::pack(s, t);
 #pragma unroll
-                for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, nb * 32, t, i, lane), ds, dq[i]);
+                for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, ln, nb * 32, t, i, lane), ds, dq[i]);
             }
         }
-        if (tile + 1 < t1) put(buf ^ 1);
+        if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
+        if (LOAD == kDma) dma_wait();
         __syncthreads();
     }
     if (r >= rows) return;
@@ -177,19 +230,21 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dq(const AttnCall c)
     for (int i = 0; i < ND; ++i) store_column<T, ALN>(out, dq[i], c.scale, 32 * i + 4 * half, c.d);
 }
 
-template <typename T, int DP, int RT, int WAVES, bool BIAS, bool ALN>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(const AttnCall c)
+template <typename T, int DP, int RT, int WAVES, bool BIAS, Load LOAD>
+__global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_dkv(const AttnCall c)
 {
     using M = Mma<T>;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
+    using D = Dma<T, DP, RT, 64 * WAVES>;
+    constexpr bool ALN = LOAD != kAny;
     constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = RT / 32, NF = 32 / M::kStep, ND = DP / 32;
-    constexpr int kTile = RT * TL::kRow, NPC = RT * TL::kPieces / NT;
+    constexpr int kTile = D::kTile, NPC = D::kCount;
     constexpr bool kDiff = BIAS || sizeof(T) == 4;
-    static_assert(RT * TL::kPieces % NT == 0 && RT <= NT, "");
+    constexpr int kStats = kDiff ? 3 : 2;
+    static_assert(RT * TL::kPieces % NT == 0 && RT <= 64, "");
     __shared__ __align__(16) char lds[4 * kTile];
-    __shared__ __align__(16) float lstat[2][3][RT];   // m, off, D
-    __shared__ __align__(16) int llimit[2][RT];
+    __shared__ __align__(16) float lstat[2][kStats][RT];   // off, D, m
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (c.m + 32 * WAVES - 1) / (32 * WAVES);
@@ -211,7 +266,85 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(const AttnCall c)
     const int begin = first * c.group / RT, end = key0 < k_len ? (q_len * c.group + RT - 1) / RT : begin;
     const int tiles = max(0, end - begin), per = (tiles + c.splits - 1) / c.splits;
     const int t0 = begin + min(tiles, split * per), t1 = min(begin + tiles, t0 + per);
+    // the first packed row that sees this lane's key
+    const int sees = c.causal ? max(0, key - k_len + q_len) * c.group : 0;
 
+    const T *qp = (const T *)c.q + b * c.sq.batch + (int64_t)hk * c.group * c.sq.head;
+    const T *gp = (const T *)c.d_o + b * c.s_do.batch + (int64_t)hk * c.group * c.s_do.head;
+    const int64_t pad = round_up_rows(rows);
+    const float *sp = c.row_stat + 3 * bh * pad;
+    const LdsPtr base = (LdsPtr)lds;
+
+    unsigned qo[LOAD == kDma ? NPC : 1], go[LOAD == kDma ? NPC : 1];
+    uint4 qr[LOAD == kDma ? 1 : NPC], gr[LOAD == kDma ? 1 : NPC];
+    float sr[kStats];
+    auto offset = [&](int row, const HeadsAt &at, int piece) {   // of a row within its tile, which begins with a whole query
+        const Packed pk = unpack(row, c.group);
+        return (unsigned)((pk.q * (int)at.row + pk.g * (int)at.head) * (int)sizeof(T) + piece * 16);
+    };
+    if constexpr (LOAD == kDma) {
+#pragma unroll
+        for (int i = 0; i < NPC; ++i) {
+            qo[i] = offset(D::row(tid, i), c.sq, D::piece(tid, i));
+            go[i] = offset(D::row(tid, i), c.s_do, D::piece(tid, i));
+        }
+        if (c.d != DP && t0 < t1) {
+            for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+        }
+    }
+    auto fetch = [&](int tile, int buf) {
+        if constexpr (LOAD == kDma) {
+            const int64_t q0 = tile * RT / c.group;
+            const char *qb = (const char *)(qp + q0 * c.sq.row), *gb = (const char *)(gp + q0 * c.s_do.row);
+            const unsigned to = lds_address(base) + 2 * buf * kTile;
+            if ((tile + 1) * RT <= q_len * c.group) {
+                D::load(qb, qo, to, tid, c.d);
+                D::load(gb, go, to + kTile, tid, c.d);
+            } else {   // the last row again beyond the end, where probabilities are zero
+                unsigned qe[NPC], ge[NPC];
+#pragma unroll
+                for (int i = 0; i < NPC; ++i) {
+                    const int row = min(D::row(tid, i), q_len * c.group - 1 - tile * RT);
+                    qe[i] = offset(row, c.sq, D::piece(tid, i));
+                    ge[i] = offset(row, c.s_do, D::piece(tid, i));
+                }
+                D::load(qb, qe, to, tid, c.d);
+                D::load(gb, ge, to + kTile, tid, c.d);
+            }
+            if (__builtin_amdgcn_readfirstlane(wave) == 0 && lane < RT) {
+                const unsigned at = __builtin_amdgcn_readfirstlane(lds_address((LdsPtr)(const char *)&lstat[buf][0][0]));
+#pragma unroll
+                for (int k = 0; k < kStats; ++k) dma4s(sp + k * pad + (int64_t)tile * RT, 4 * lane, at + k * RT * 4);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) {
+                const int p = tid + i * NT, pc = p % TL::kPieces;
+                const Packed pk = unpack(min(tile * RT + p / TL::kPieces, q_len * c.group - 1), c.group);
+                qr[i] = load_piece<T, ALN>(qp + (int64_t)pk.q * c.sq.row + pk.g * c.sq.head, pc, c.d);
+                gr[i] = load_piece<T, ALN>(gp + (int64_t)pk.q * c.s_do.row + pk.g * c.s_do.head, pc, c.d);
+            }
+            if (tid < RT)
+#pragma unroll
+                for (int k = 0; k < kStats; ++k) sr[k] = sp[k * pad + tile * RT + tid];
+        }
+    };
+    auto put = [&](int buf) {
+        if constexpr (LOAD != kDma) {
+#pragma unroll
+            for (int i = 0; i < NPC; ++i) {
+                const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
+                *(uint4 *)(lds + (2 * buf) * kTile + at) = qr[i];
+                *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = gr[i];
+            }
+            if (tid < RT)
+#pragma unroll
+                for (int k = 0; k < kStats; ++k) lstat[buf][k][tid] = sr[k];
+        }
+    };
+
+    if (t0 < t1) fetch(t0, 0);
     Frag k[NS], v[NS];
     {
         const T *rk = (const T *)c.k + b * c.sk.batch + (int64_t)key * c.sk.row + hk * c.sk.head;
@@ -224,88 +357,51 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(const AttnCall c)
         }
     }
     const float unit = kDiff ? kLog2eF : c.scale * kLog2eF;
-    const T *qp = (const T *)c.q + b * c.sq.batch + (int64_t)hk * c.group * c.sq.head;
-    const T *gp = (const T *)c.d_o + b * c.s_do.batch + (int64_t)hk * c.group * c.s_do.head;
-
-    uint4 qr[NPC], gr[NPC];
-    RowStat st = {0.0f, INFINITY};
-    float delta = 0.0f;
-    int limit = 0;
-    auto fetch = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < NPC; ++i) {
-            const int p = tid + i * NT, row = tile * RT + p / TL::kPieces, pc = p % TL::kPieces;
-            const Packed pk = unpack(row, c.group);
-            const bool there = pk.q < q_len;
-            qr[i] = there ? load_piece<T, ALN>(qp + (int64_t)pk.q * c.sq.row + pk.g * c.sq.head, pc, c.d) : make_uint4(0, 0, 0, 0);
-            gr[i] = there ? load_piece<T, ALN>(gp + (int64_t)pk.q * c.s_do.row + pk.g * c.s_do.head, pc, c.d) : make_uint4(0, 0, 0, 0);
-        }
-        if (tid < RT) {
-            const Packed pk = unpack(tile * RT + tid, c.group);
-            st = {0.0f, INFINITY};
-            delta = 0.0f;
-            limit = 0;
-            if (pk.q < q_len) {
-                const float2 w = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
-                st = row_stat<kDiff>(w.x, w.y);
-                delta = c.delta[bh * rows + tile * RT + tid];
-                limit = c.causal ? pk.q + k_len - q_len + 1 : c.m;
-            }
-        }
-    };
-    auto put = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < NPC; ++i) {
-            const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
-            *(uint4 *)(lds + (2 * buf) * kTile + at) = qr[i];
-            *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = gr[i];
-        }
-        if (tid < RT) {
-            lstat[buf][0][tid] = st.m;
-            lstat[buf][1][tid] = st.off;
-            lstat[buf][2][tid] = delta;
-            llimit[buf][tid] = limit;
-        }
-    };
+    const typename TL::Lanes ln = TL::lanes(lane);
 
     f32x16 dk[ND], dv[ND];
     float db = 0.0f;
 #pragma unroll
     for (int i = 0; i < ND; ++i) dk[i] = dv[i] = (f32x16)(0.0f);
-    if (t0 < t1) {
-        fetch(t0);
-        put(0);
-    }
+    if (t0 < t1) put(0);
+    dma_wait();
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
     for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
-        const char *lq = lds + 2 * buf * kTile, *lg = lq + kTile;
-        if (tile + 1 < t1) fetch(tile + 1);
-        // the tile's first row sees fewer keys than the others
-        const bool masked = c.causal && tile * RT / c.group + k_len - q_len + 1 < key0 + 32 * WAVES;
+        const LdsPtr lq = base + 2 * buf * kTile, lg = lq + kTile;
+        if (tile + 1 < t1) fetch(tile + 1, buf ^ 1);
+        const bool masked = __any(tile * RT < sees);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             f32x16 s = (f32x16)(0.0f), dp = (f32x16)(0.0f);
 #pragma unroll
             for (int t = 0; t < NS; ++t) {
-                s = M::mma(TL::rows(lq, nb * 32, t, lane), k[t], s);
-                dp = M::mma(TL::rows(lg, nb * 32, t, lane), v[t], dp);
+                s = M::mma(TL::rows(lq, ln, nb * 32, t), k[t], s);
+                dp = M::mma(TL::rows(lg, ln, nb * 32, t), v[t], dp);
+            }
+            if constexpr (BIAS) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], c.scale, bias);
+            }
+            if (masked) {
+                const int base = tile * RT + nb * 32 + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = base + 8 * (i / 4) + i % 4 >= sees ? s[i] : -INFINITY;
             }
             f32x16 p;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int at = nb * 32 + 8 * u + 4 * half;
-                const f32x4 off = *(const f32x4 *)&lstat[buf][1][at], dl = *(const f32x4 *)&lstat[buf][2][at];
+                const f32x4 off = *(const f32x4 *)&lstat[buf][0][at], dl = *(const f32x4 *)&lstat[buf][1][at];
                 f32x4 m;
-                if (kDiff) m = *(const f32x4 *)&lstat[buf][0][at];
+                if (kDiff) m = *(const f32x4 *)&lstat[buf][kStats - 1][at];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * u + j;
-                    const float d = BIAS ? fmaf(s[i], c.scale, bias) - m[j] : kDiff ? fmaf(s[i], c.scale, -m[j]) : s[i];
-                    float e = __builtin_amdgcn_exp2f(fmaf(d, unit, -off[j]));
-                    if (masked && key >= llimit[buf][at + j]) e = 0.0f;
-                    p[i] = e;
-                    s[i] = e * (dp[i] - dl[j]);
+                    const float d = BIAS ? s[i] - m[j] : kDiff ? fmaf(s[i], c.scale, -m[j]) : s[i];
+                    p[i] = __builtin_amdgcn_exp2f(fmaf(d, unit, -off[j]));
+                    s[i] = p[i] * (dp[i] - dl[j]);
                     if (BIAS) db += s[i];
                 }
             }
@@ -314,12 +410,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_attn_dkv(const AttnCall c)
                 const Frag pf = M::pack(p, t), sf = M::pack(s, t);
 #pragma unroll
                 for (int i = 0; i < ND; ++i) {
-                    dv[i] = M::mma(TL::cols(lg, nb * 32, t, i, lane), pf, dv[i]);
-                    dk[i] = M::mma(TL::cols(lq, nb * 32, t, i, lane), sf, dk[i]);
+                    dv[i] = M::mma(TL::cols(lg, ln, nb * 32, t, i, lane), pf, dv[i]);
+                    dk[i] = M::mma(TL::cols(lq, ln, nb * 32, t, i, lane), sf, dk[i]);
                 }
             }
         }
-        if (tile + 1 < t1) put(buf ^ 1);
+        if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
+        if (LOAD == kDma) dma_wait();
         __syncthreads();
     }
     if (BIAS) db = across_halves_sum(db);
@@ -388,11 +485,11 @@ template <typename T> __global__ __launch_bounds__(256) void k_attn_dbias(const 
 }
 
 template <typename T, int DP>
-fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool aligned)
+fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Load rows_load)
 {
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, RT = sizeof(T) == 2 && DP < 128 ? 64 : 32;
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32, RT = row_tile(sizeof(T));
     Arena A;
-    a.delta = (float *)(ws + A.take(p.delta_bytes));
+    a.row_stat = (float *)(ws + A.take(p.stat_bytes));
     float *dq_part = (float *)(ws + A.take(p.dq_bytes)), *dkv_part = (float *)(ws + A.take(p.dkv_bytes));
     a.dbias_part = (float *)(ws + A.take(p.dbias_bytes));
     const int64_t heads = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.n * a.group;
@@ -401,11 +498,12 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool aligned)
     if (p.q_grid) {
         const unsigned grid = (unsigned)p.q_grid;
         if (a.bias) {
-            if (aligned) k_attn_dq<T, DP, KT, 4, true, true><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dq<T, DP, KT, 4, true, false><<<grid, 256, 0, c->stream>>>(a);
+            if (keys != kAny) k_attn_dq<T, DP, KT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dq<T, DP, KT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
         } else {
-            if (aligned) k_attn_dq<T, DP, KT, 4, false, true><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dq<T, DP, KT, 4, false, false><<<grid, 256, 0, c->stream>>>(a);
+            if (keys == kDma) k_attn_dq<T, DP, KT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
+            else if (keys == kVec) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dq<T, DP, KT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
         if (a.splits > 1) k_attn_grad_join<T, DP, false><<<(unsigned)ceil_div(heads * rows, 4), 256, 0, c->stream>>>(a);
     }
@@ -414,11 +512,13 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool aligned)
     if (p.k_grid) {
         const unsigned grid = (unsigned)p.k_grid;
         if (a.bias) {
-            if (aligned) k_attn_dkv<T, DP, RT, 4, true, true><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dkv<T, DP, RT, 4, true, false><<<grid, 256, 0, c->stream>>>(a);
+            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, true, kDma><<<grid, 256, 0, c->stream>>>(a);
+            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dkv<T, DP, RT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
         } else {
-            if (aligned) k_attn_dkv<T, DP, RT, 4, false, true><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dkv<T, DP, RT, 4, false, false><<<grid, 256, 0, c->stream>>>(a);
+            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
+            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
+            else k_attn_dkv<T, DP, RT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
         if (a.splits > 1) k_attn_grad_join<T, DP, true><<<(unsigned)ceil_div(heads * a.m, 4), 256, 0, c->stream>>>(a);
         if (a.dbias) k_attn_dbias<T><<<(unsigned)ceil_div((int64_t)a.batch * a.m, 256), 256, 0, c->stream>>>(a);
@@ -427,13 +527,13 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool aligned)
     return FS_OK;
 }
 
-template <typename T> fs_status by_width(Ctx *c, const AttnCall &a, const AttnGradPlan &p, char *ws, bool aligned)
+template <typename T> fs_status by_width(Ctx *c, const AttnCall &a, const AttnGradPlan &p, char *ws, Load keys, Load rows)
 {
     switch ((a.d + 31) / 32) {
-    case 1: return run<T, 32>(c, a, p, ws, aligned);
-    case 2: return run<T, 64>(c, a, p, ws, aligned);
-    case 3: return run<T, 96>(c, a, p, ws, aligned);
-    default: return run<T, 128>(c, a, p, ws, aligned);
+    case 1: return run<T, 32>(c, a, p, ws, keys, rows);
+    case 2: return run<T, 64>(c, a, p, ws, keys, rows);
+    case 3: return run<T, 96>(c, a, p, ws, keys, rows);
+    default: return run<T, 128>(c, a, p, ws, keys, rows);
     }
 }
 
@@ -445,12 +545,12 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
     const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads, dp = round_up(a.d, 32);
     const int64_t want = 2 * (int64_t)c->num_cu;
     const int64_t qb = ceil_div(rows, 128) * heads, kb = ceil_div(a.m, 128) * heads;
-    const int64_t kt = ceil_div(a.m, f32 ? 32 : 64), rt = ceil_div(rows, 32);
+    const int64_t kt = ceil_div(a.m, f32 ? 32 : 64), rt = ceil_div(rows, row_tile(f32 ? 4 : 2));
     p.q_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(qb, 1), kt / 4));
-    p.k_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(kb, 1), rt / 8));
+    p.k_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(kb, 1), rt / 4));
     p.q_grid = qb * p.q_splits;
     p.k_grid = kb * p.k_splits;
-    p.delta_bytes = (size_t)(heads * rows) * 4;
+    p.stat_bytes = (size_t)(heads * round_up(rows, kRowBlock)) * 12;
     p.dq_bytes = p.q_splits > 1 ? (size_t)(heads * rows * dp * p.q_splits) * 4 : 0;
     p.dkv_bytes = p.k_splits > 1 ? (size_t)(heads * a.m * dp * 2 * p.k_splits) * 4 : 0;
     p.dbias_bytes = a.dbias ? (size_t)(heads * a.m * p.k_splits) * 4 : 0;
@@ -459,7 +559,14 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
 
 fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool f32, bool aligned)
 {
-    return f32 ? by_width<float>(c, a, p, ws, aligned) : by_width<__bf16>(c, a, p, ws, aligned);
+    const int es = f32 ? 4 : 2;
+    const int64_t kmost = std::max(a.sk.row, a.sv.row) * es * 64;
+    const Load keys = !aligned ? kAny : kmost < (int64_t(1) << 31) ? kDma : kVec;
+    // tiles of rows begin with a whole query
+    const int rt = row_tile(es);
+    const int64_t rmost = (std::max(a.sq.row, a.s_do.row) * rt / a.group + std::max(a.sq.head, a.s_do.head) * a.group) * es;
+    const Load rows = !aligned ? kAny : rt % a.group == 0 && rmost < (int64_t(1) << 31) ? kDma : kVec;
+    return f32 ? by_width<float>(c, a, p, ws, keys, rows) : by_width<__bf16>(c, a, p, ws, keys, rows);
 }
 
 }  // namespace fs
