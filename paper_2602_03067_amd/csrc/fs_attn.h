@@ -221,11 +221,34 @@ __device__ inline Packed unpack(int r, int group)
     return {q, r - q * group};
 }
 
-// Workgroups that share an XCD's L2 (ids equal mod 8) take consecutive work.
-__device__ inline int xcd_order(int id, int total)
+// What a workgroup works on.  Workgroups that share an XCD's L2 (ids equal mod 8) take consecutive work of the order (set and kv head;
+// block of rows or keys; split).  Under a causal line blocks are of unequal length, and consecutive blocks would give one XCD the
+// long half of a head and its neighbour the short one: `rank` counts blocks from the longest, and
+//  - where every XCD has whole heads, blocks come by rank, the longest first;
+//  - where a head has a whole number of XCDs, each takes every so many-th of them;
+//  - otherwise they alternate between long and short ones.
+struct Work {
+    int split, rank, hk, b;
+};
+__device__ inline Work work_of(int id, int total, int splits, int blocks, int kv_heads, bool causal)
 {
-    const int x = id & 7, j = id >> 3, per = total >> 3, more = total & 7;
-    return x * per + (x < more ? x : more) + j;
+    const int x = id & 7, per = total >> 3, more = total & 7;
+    id = x * per + (x < more ? x : more) + (id >> 3);
+    Work w;
+    w.split = id % splits;
+    id /= splits;
+    int j = id % blocks;
+    id /= blocks;
+    const int heads = total / (splits * blocks);
+    if (causal && heads % 8 != 0) {
+        const int share = heads < 8 && 8 % heads == 0 ? 8 / heads : 0;
+        if (share && blocks % share == 0) j = j % (blocks / share) * share + j / (blocks / share);
+        else j = j & 1 ? blocks - 1 - j / 2 : j / 2;
+    }
+    w.rank = j;
+    w.hk = id % kv_heads;
+    w.b = id / kv_heads;
+    return w;
 }
 
 // how a forward pass is launched

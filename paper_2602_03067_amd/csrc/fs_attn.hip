@@ -34,12 +34,8 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int split = id % c.splits;
-    id /= c.splits;
-    const int blk = blocks - 1 - id % blocks;   // (causal: the long ones first)
-    id /= blocks;
-    const int hk = id % c.kv_heads, b = id / c.kv_heads;
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
+    const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
     const int q_len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
@@ -155,9 +151,9 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const f32x4 w = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * g + 4 * half];
+                    const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * g + 4 * half];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], c.scale, w[j]);
+                    for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], c.scale, add[j]);
                 }
         }
         if (__any(limit < (tile + 1) * KT)) {

@@ -50,12 +50,8 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int split = id % c.splits;
-    id /= c.splits;
-    const int blk = blocks - 1 - id % blocks;   // (causal: the long ones first)
-    id /= blocks;
-    const int hk = id % c.kv_heads, b = id / c.kv_heads;
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
+    const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
     const int q_len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
@@ -187,9 +183,9 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
             if constexpr (BIAS) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const f32x4 w = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * u + 4 * half];
+                    const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * u + 4 * half];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], c.scale, w[j]);
+                    for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], c.scale, add[j]);
                 }
             }
             if (masked) {
@@ -248,12 +244,8 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (c.m + 32 * WAVES - 1) / (32 * WAVES);
-    int id = xcd_order(blockIdx.x, gridDim.x);
-    const int split = id % c.splits;
-    id /= c.splits;
-    const int blk = id % blocks;   // (causal: the long ones first)
-    id /= blocks;
-    const int hk = id % c.kv_heads, b = id / c.kv_heads;
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
+    const int split = w.split, blk = w.rank, hk = w.hk, b = w.b;
     const int64_t bh = (int64_t)b * c.kv_heads + hk;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
@@ -547,7 +539,8 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
     const int64_t qb = ceil_div(rows, 128) * heads, kb = ceil_div(a.m, 128) * heads;
     const int64_t kt = ceil_div(a.m, f32 ? 32 : 64), rt = ceil_div(rows, row_tile(f32 ? 4 : 2));
     p.q_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(qb, 1), kt / 4));
-    p.k_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(kb, 1), rt / 4));
+    // (under a causal line blocks are of unequal length: twice as many, so that short ones fill up behind long ones)
+    p.k_splits = (int)std::max<int64_t>(1, std::min((a.causal ? 2 : 1) * want / std::max<int64_t>(kb, 1), rt / 4));
     p.q_grid = qb * p.q_splits;
     p.k_grid = kb * p.k_splits;
     p.stat_bytes = (size_t)(heads * round_up(rows, kRowBlock)) * 12;
