@@ -10,10 +10,12 @@ namespace fs {
 namespace {
 
 constexpr float kLog2eF = 1.44269504088896340736f;
-// Probabilities are taken below a reference that follows the row's maximum at a distance of at most 2^8: the accumulators are
-// rescaled only where the maximum has grown by more.  Sums stay far inside a float, and a bf16 probability has the same
-// relative rounding at any size.
-constexpr float kSlack = 8.0f;
+// Probabilities are taken below a reference: the row's maximum over the first tile in which it sees a key.  As long as no later score
+// exceeds it by more than 2^kSlack, and that is the rule, nothing is ever rescaled: sums and accumulators are floats, which 2^30 leaves
+// room enough, and a bf16 probability has the same relative rounding at any size.  A wave that meets a larger score goes on in a
+// second loop, which follows the maximum and rescales in every tile.  (With the rescaling in a branch of one loop the compiler
+// keeps two copies of the accumulators and moves them to and fro.)
+constexpr float kSlack = 30.0f;
 
 // waves per SIMD: what registers allow without spills
 constexpr int min_waves(size_t elem, int dp) { return elem == 4 && dp >= 96 ? 1 : 2; }
@@ -134,12 +136,10 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
     dma_wait();   // (of q as well: not inside the loop, where it would wait for the next tile)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
-    for (int tile = t0; tile < t1; ++tile) {
+    // scores of a tile; returns the row's largest
+    auto scores = [&](int tile, f32x16 (&s)[NB]) {
         const int buf = (tile - t0) & 1;
-        const LdsPtr lk = base + 2 * buf * kTile, lv = lk + kTile;
-        if (tile + 1 < t1) fetch(tile + 1, buf ^ 1);
-
-        f32x16 s[NB];
+        const LdsPtr lk = base + 2 * buf * kTile;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             s[nb] = (f32x16)(0.0f);
@@ -157,27 +157,23 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
                 }
         }
         if (__any(limit < (tile + 1) * KT)) {
-            const int base = tile * KT + 4 * half;
+            const int key0 = tile * KT + 4 * half;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    s[nb][i] = base + nb * 32 + 8 * (i / 4) + i % 4 < limit ? s[nb][i] : -INFINITY;
+                    s[nb][i] = key0 + nb * 32 + 8 * (i / 4) + i % 4 < limit ? s[nb][i] : -INFINITY;
         }
         float mx = -INFINITY;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[nb][i]);
-        mx = across_halves_max(mx);
-        top = fmaxf(top, mx);
-        if (__any((mx - ref) * unit > kSlack)) {   // (the first keys of a row: from minus infinity)
-            const float next = fmaxf(ref, mx), f = next == ref ? 1.0f : __builtin_amdgcn_exp2f((ref - next) * unit);
-            ref = next;
-            sum *= f;
-#pragma unroll
-            for (int i = 0; i < ND; ++i) o[i] *= f;
-        }
+        return across_halves_max(mx);
+    };
+    // their exponentials into the sum and, times the values, into the accumulators
+    auto accumulate = [&](int tile, f32x16 (&s)[NB]) {
+        const LdsPtr lv = base + 2 * ((tile - t0) & 1) * kTile + kTile;
         const float safe = ref == -INFINITY ? 0.0f : ref, off = safe * unit;
         float part = 0.0f;
 #pragma unroll
@@ -199,9 +195,38 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
 #pragma unroll
                 for (int i = 0; i < ND; ++i) o[i] = M::mma(TL::cols(lv, ln, nb * 32, t, i, lane), p, o[i]);
             }
-        if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
+    };
+    auto next_tile = [&](int tile) {
+        if (LOAD != kDma && tile + 1 < t1) put((tile + 1 - t0) & 1);
         if (LOAD == kDma) dma_wait();
         __syncthreads();
+    };
+    int tile = t0;
+    bool fetched = false;
+    for (; tile < t1; ++tile) {
+        if (tile + 1 < t1) fetch(tile + 1, (tile + 1 - t0) & 1);
+        f32x16 s[NB];
+        const float mx = scores(tile, s);
+        ref = ref == -INFINITY ? mx : ref;
+        fetched = __any((mx - ref) * unit > kSlack);
+        if (fetched) break;
+        top = fmaxf(top, mx);
+        accumulate(tile, s);
+        next_tile(tile);
+    }
+    for (; tile < t1; ++tile) {
+        if (!fetched && tile + 1 < t1) fetch(tile + 1, (tile + 1 - t0) & 1);
+        fetched = false;
+        f32x16 s[NB];
+        const float mx = scores(tile, s), next = fmaxf(ref, mx);
+        const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f((ref - next) * unit);   // (from minus infinity: 0)
+        top = fmaxf(top, mx);
+        ref = next;
+        sum *= f;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) o[i] *= f;
+        accumulate(tile, s);
+        next_tile(tile);
     }
 
     sum = across_halves_sum(sum);
