@@ -125,19 +125,38 @@ __device__ inline unsigned lds_address(LdsPtr p) { return (unsigned)(uintptr_t)p
 enum Load { kDma, kVec, kAny };
 
 // Direct loads of a tile of ROWS rows by NT threads: LDS takes consecutive 16-byte pieces of consecutive lanes, so a lane fetches the piece
-// that the permutation puts there.  Pieces beyond d are left alone (zeroed once).
+// that the permutation puts there.  Pieces beyond d are left alone (zeroed once).  Where a round of the threads is a whole number of rows
+// that the permutation treats alike, a lane's offset is the same in every round, and the rounds differ in their uniform base.
 template <typename T, int DP, int ROWS, int NT> struct Dma {
     using TL = Tile<T, DP>;
     static constexpr int kCount = ROWS * TL::kPieces / NT, kTile = ROWS * TL::kRow;
+    static constexpr int kRound = NT / TL::kPieces;   // rows
+    static constexpr bool kAlike = NT % TL::kPieces == 0 && kRound % 8 == 0;
+    static constexpr int kOffsets = kAlike ? 1 : kCount;
     static __device__ inline int row(int tid, int i) { return (tid + i * NT) / TL::kPieces; }
     static __device__ inline int piece(int tid, int i) { return ((tid + i * NT) % TL::kPieces) ^ TL::swz(row(tid, i)); }
-    // base: of the tile's first row (uniform); off[i]: bytes from there; lds: of the tile (uniform)
-    static __device__ inline void load(const char *base, const unsigned (&off)[kCount], unsigned lds, int tid, int d)
+    // base: of the tile's first row (uniform); off: bytes from there, of each round or of the first; round: bytes between rounds;
+    // rows from `count` on are left alone
+    static __device__ inline void load(const char *base, const unsigned (&off)[kOffsets], int64_t round, unsigned lds, int tid, int d, int count)
     {
         const unsigned to = __builtin_amdgcn_readfirstlane(lds + (tid >> 6) * 1024);
+        if (d == DP && count >= ROWS) {
 #pragma unroll
-        for (int i = 0; i < kCount; ++i)
-            if (d == DP || piece(tid, i) * Mma<T>::kPiece < d) dma16s(base, off[i], to + i * NT * 16);
+            for (int i = 0; i < kCount; ++i) dma16s(kAlike ? base + i * round : base, off[kAlike ? 0 : i], to + i * NT * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCount; ++i)
+                if (piece(tid, i) * Mma<T>::kPiece < d && row(tid, i) < count)
+                    dma16s(kAlike ? base + i * round : base, off[kAlike ? 0 : i], to + i * NT * 16);
+        }
+    }
+    // What no load writes is zero, or a row of an earlier tile (which no probability counts): zeroed before the first tile where
+    // there are pieces beyond d, or where the last tile, of `count` rows, has no tile before it in its buffer.
+    static __device__ inline void clear(char *lds, int tid, int d, int count, int tiles)
+    {
+        if (d == DP && (count >= ROWS || tiles > 2)) return;
+        for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
+        __syncthreads();
     }
 };
 __device__ inline void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }

@@ -57,39 +57,24 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
     const LdsPtr base = (LdsPtr)lds;
 
     // what a thread fetches of a tile
-    unsigned ko[LOAD == kDma ? NPC : 1], vo[LOAD == kDma ? NPC : 1];
+    unsigned ko[D::kOffsets], vo[D::kOffsets];
     uint4 kr[LOAD == kDma ? 1 : NPC], vr[LOAD == kDma ? 1 : NPC];
     float br = 0.0f;
     if constexpr (LOAD == kDma) {
 #pragma unroll
-        for (int i = 0; i < NPC; ++i) {
+        for (int i = 0; i < D::kOffsets; ++i) {
             ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
             vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
         }
-        if (c.d != DP && t0 < t1) {   // pieces that no load writes
-            for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
-            __syncthreads();
-        }
+        if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KT, t1 - t0);
     }
     // kDma: the whole way; otherwise to registers
     auto fetch = [&](int tile, int buf) {
         if constexpr (LOAD == kDma) {
             const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            if ((tile + 1) * KT <= k_len) {
-                D::load(kb, ko, to, tid, c.d);
-                D::load(vb, vo, to + kTile, tid, c.d);
-            } else {   // the last row again beyond the end
-                unsigned ke[NPC], ve[NPC];
-#pragma unroll
-                for (int i = 0; i < NPC; ++i) {
-                    const int row = min(D::row(tid, i), k_len - 1 - tile * KT);
-                    ke[i] = (unsigned)(row * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
-                    ve[i] = (unsigned)(row * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
-                }
-                D::load(kb, ke, to, tid, c.d);
-                D::load(vb, ve, to + kTile, tid, c.d);
-            }
+            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(T), to, tid, c.d, k_len - tile * KT);
+            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(T), to + kTile, tid, c.d, k_len - tile * KT);
         } else {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {

@@ -70,38 +70,23 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
     const LdsPtr base = (LdsPtr)lds;
 
     // (tiles of keys as in k_attn)
-    unsigned ko[LOAD == kDma ? NPC : 1], vo[LOAD == kDma ? NPC : 1];
+    unsigned ko[D::kOffsets], vo[D::kOffsets];
     uint4 kr[LOAD == kDma ? 1 : NPC], vr[LOAD == kDma ? 1 : NPC];
     float br = 0.0f;
     if constexpr (LOAD == kDma) {
 #pragma unroll
-        for (int i = 0; i < NPC; ++i) {
+        for (int i = 0; i < D::kOffsets; ++i) {
             ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
             vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
         }
-        if (c.d != DP && t0 < t1) {
-            for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
-            __syncthreads();
-        }
+        if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KT, t1 - t0);
     }
     auto fetch = [&](int tile, int buf) {
         if constexpr (LOAD == kDma) {
             const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            if ((tile + 1) * KT <= k_len) {
-                D::load(kb, ko, to, tid, c.d);
-                D::load(vb, vo, to + kTile, tid, c.d);
-            } else {
-                unsigned ke[NPC], ve[NPC];
-#pragma unroll
-                for (int i = 0; i < NPC; ++i) {
-                    const int row = min(D::row(tid, i), k_len - 1 - tile * KT);
-                    ke[i] = (unsigned)(row * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
-                    ve[i] = (unsigned)(row * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
-                }
-                D::load(kb, ke, to, tid, c.d);
-                D::load(vb, ve, to + kTile, tid, c.d);
-            }
+            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(T), to, tid, c.d, k_len - tile * KT);
+            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(T), to + kTile, tid, c.d, k_len - tile * KT);
         } else {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
@@ -267,7 +252,7 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
     const float *sp = c.row_stat + 3 * bh * pad;
     const LdsPtr base = (LdsPtr)lds;
 
-    unsigned qo[LOAD == kDma ? NPC : 1], go[LOAD == kDma ? NPC : 1];
+    unsigned qo[D::kOffsets], go[D::kOffsets];
     uint4 qr[LOAD == kDma ? 1 : NPC], gr[LOAD == kDma ? 1 : NPC];
     float sr[kStats];
     auto offset = [&](int row, const HeadsAt &at, int piece) {   // of a row within its tile, which begins with a whole query
@@ -276,34 +261,20 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
     };
     if constexpr (LOAD == kDma) {
 #pragma unroll
-        for (int i = 0; i < NPC; ++i) {
+        for (int i = 0; i < D::kOffsets; ++i) {
             qo[i] = offset(D::row(tid, i), c.sq, D::piece(tid, i));
             go[i] = offset(D::row(tid, i), c.s_do, D::piece(tid, i));
         }
-        if (c.d != DP && t0 < t1) {
-            for (int i = tid; i < 4 * kTile / 16; i += NT) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
-            __syncthreads();
-        }
+        if (t0 < t1) D::clear(lds, tid, c.d, q_len * c.group - (t1 - 1) * RT, t1 - t0);
     }
     auto fetch = [&](int tile, int buf) {
         if constexpr (LOAD == kDma) {
             const int64_t q0 = tile * RT / c.group;
             const char *qb = (const char *)(qp + q0 * c.sq.row), *gb = (const char *)(gp + q0 * c.s_do.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            if ((tile + 1) * RT <= q_len * c.group) {
-                D::load(qb, qo, to, tid, c.d);
-                D::load(gb, go, to + kTile, tid, c.d);
-            } else {   // the last row again beyond the end, where probabilities are zero
-                unsigned qe[NPC], ge[NPC];
-#pragma unroll
-                for (int i = 0; i < NPC; ++i) {
-                    const int row = min(D::row(tid, i), q_len * c.group - 1 - tile * RT);
-                    qe[i] = offset(row, c.sq, D::piece(tid, i));
-                    ge[i] = offset(row, c.s_do, D::piece(tid, i));
-                }
-                D::load(qb, qe, to, tid, c.d);
-                D::load(gb, ge, to + kTile, tid, c.d);
-            }
+            const int queries = D::kRound / c.group, left = q_len * c.group - tile * RT;   // (a round is whole queries: see launch_attn_grad)
+            D::load(qb, qo, queries * c.sq.row * (int)sizeof(T), to, tid, c.d, left);
+            D::load(gb, go, queries * c.s_do.row * (int)sizeof(T), to + kTile, tid, c.d, left);
             if (__builtin_amdgcn_readfirstlane(wave) == 0 && lane < RT) {
                 const unsigned at = __builtin_amdgcn_readfirstlane(lds_address((LdsPtr)(const char *)&lstat[buf][0][0]));
 #pragma unroll
@@ -366,12 +337,11 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
         const bool masked = __any(tile * RT < sees);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
+            // one after the other: 192 registers of keys, values and accumulators at d = 128 leave room for two of the three products
+            // that a block is made of
             f32x16 s = (f32x16)(0.0f), dp = (f32x16)(0.0f);
 #pragma unroll
-            for (int t = 0; t < NS; ++t) {
-                s = M::mma(TL::rows(lq, ln, nb * 32, t), k[t], s);
-                dp = M::mma(TL::rows(lg, ln, nb * 32, t), v[t], dp);
-            }
+            for (int t = 0; t < NS; ++t) s = M::mma(TL::rows(lq, ln, nb * 32, t), k[t], s);
             if constexpr (BIAS) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], c.scale, bias);
@@ -381,31 +351,47 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = base + 8 * (i / 4) + i % 4 >= sees ? s[i] : -INFINITY;
             }
-            f32x16 p;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int at = nb * 32 + 8 * u + 4 * half;
-                const f32x4 off = *(const f32x4 *)&lstat[buf][0][at], dl = *(const f32x4 *)&lstat[buf][1][at];
+                const f32x4 off = *(const f32x4 *)&lstat[buf][0][at];
                 f32x4 m;
                 if (kDiff) m = *(const f32x4 *)&lstat[buf][kStats - 1][at];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * u + j;
                     const float d = BIAS ? s[i] - m[j] : kDiff ? fmaf(s[i], c.scale, -m[j]) : s[i];
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(d, unit, -off[j]));
-                    s[i] = p[i] * (dp[i] - dl[j]);
+                    s[i] = __builtin_amdgcn_exp2f(fmaf(d, unit, -off[j]));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < NF; ++t) {
+                const Frag pf = M::pack(s, t);
+#pragma unroll
+                for (int i = 0; i < ND; ++i) dv[i] = M::mma(TL::cols(lg, ln, nb * 32, t, i, lane), pf, dv[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < NS; ++t) dp = M::mma(TL::rows(lg, ln, nb * 32, t), v[t], dp);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const f32x4 dl = *(const f32x4 *)&lstat[buf][1][nb * 32 + 8 * u + 4 * half];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 4 * u + j;
+                    s[i] *= dp[i] - dl[j];
                     if (BIAS) db += s[i];
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < NF; ++t) {
-                const Frag pf = M::pack(p, t), sf = M::pack(s, t);
+                const Frag sf = M::pack(s, t);
 #pragma unroll
-                for (int i = 0; i < ND; ++i) {
-                    dv[i] = M::mma(TL::cols(lg, ln, nb * 32, t, i, lane), pf, dv[i]);
-                    dk[i] = M::mma(TL::cols(lq, ln, nb * 32, t, i, lane), sf, dk[i]);
-                }
+                for (int i = 0; i < ND; ++i) dk[i] = M::mma(TL::cols(lq, ln, nb * 32, t, i, lane), sf, dk[i]);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
         if (LOAD == kDma) dma_wait();
@@ -555,10 +541,10 @@ fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, 
     const int es = f32 ? 4 : 2;
     const int64_t kmost = std::max(a.sk.row, a.sv.row) * es * 64;
     const Load keys = !aligned ? kAny : kmost < (int64_t(1) << 31) ? kDma : kVec;
-    // tiles of rows begin with a whole query
-    const int rt = row_tile(es);
+    // tiles of rows, and the rounds that load them, begin with a whole query
+    const int rt = row_tile(es), dp = (int)round_up(a.d, 32), round = dp == 96 ? rt : std::min(rt, 256 * 16 / dp / es);
     const int64_t rmost = (std::max(a.sq.row, a.s_do.row) * rt / a.group + std::max(a.sq.head, a.s_do.head) * a.group) * es;
-    const Load rows = !aligned ? kAny : rt % a.group == 0 && rmost < (int64_t(1) << 31) ? kDma : kVec;
+    const Load rows = !aligned ? kAny : rt % a.group == 0 && round % a.group == 0 && rmost < (int64_t(1) << 31) ? kDma : kVec;
     return f32 ? by_width<float>(c, a, p, ws, keys, rows) : by_width<__bf16>(c, a, p, ws, keys, rows);
 }
 
