@@ -11,6 +11,7 @@ import ctypes
 import os
 from typing import Optional, Tuple
 
+import numpy as np
 import torch  # loaded first so that the library binds to the same HIP runtime as torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -565,6 +566,8 @@ class AdamW:
                 setattr(entry, field, t.data_ptr())
         for entry, p in zip(self._table, self.params):
             entry.n = p.numel()
+        self._sizes = [p.numel() for p in self.params]
+        self._at = np.frombuffer(self._table, dtype=np.int64).reshape(len(self.params), 8)   # (the table's addresses; g is the second)
         self._args = FsAdamwArgs(p_dtype=_DTYPES[self.p_dtype], state_bits=state_bits)
 
     def step(self, grads, grad_scale: Optional[torch.Tensor] = None) -> None:
@@ -575,10 +578,10 @@ class AdamW:
         kind = grads[0].dtype
         if kind not in _DTYPES:
             raise TypeError("gradients must be float32 or bfloat16")
-        for entry, g in zip(self._table, grads):
-            if not g.is_cuda or g.dtype != kind or not g.is_contiguous() or g.numel() != entry.n:
+        for g, n in zip(grads, self._sizes):
+            if g.numel() != n or g.dtype is not kind or not g.is_cuda or not g.is_contiguous():
                 raise TypeError("a gradient does not fit its weights")
-            entry.g = g.data_ptr()
+        self._at[:, 1] = [g.data_ptr() for g in grads]
         a = self._args
         a.lr, (a.beta1, a.beta2), a.eps, a.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
         a.step, a.g_dtype = self.step_count + 1, _DTYPES[kind]

@@ -240,35 +240,66 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
     }
 }
 
-// Merge of the splits: a wave takes a packed row, a lane two coordinates.
-template <typename T, int DP>
+// Merge of the splits.  A thread takes four coordinates of a packed row and every G-th split, four splits' loads at a time; G groups of
+// threads share a row and meet in LDS.
+template <typename T, int DP, int G>
 __global__ __launch_bounds__(256) void k_attn_join(const AttnCall c)
 {
-    const int rows = c.n * c.group, lane = threadIdx.x & 63;
-    const int64_t total = (int64_t)c.batch * c.kv_heads * rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= total) return;
-    float top = -INFINITY;
-    for (int s = 0; s < c.splits; ++s) top = fmaxf(top, c.part_stat[(s * total + at) * 4]);
-    const float safe = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, acc[(DP + 63) / 64] = {};
-    for (int s = 0; s < c.splits; ++s) {
-        const f32x4 st = *(const f32x4 *)(c.part_stat + (s * total + at) * 4);
-        if (st[1] == -INFINITY) continue;   // no key of this split
-        const float f = __builtin_amdgcn_exp2f((st[1] - safe) * kLog2eF);
-        sum = fmaf(st[2], f, sum);
+    constexpr int W = DP / 4, R = 256 / (W * G);   // threads of a group, rows of a workgroup
+    __shared__ f32x4 lacc[G > 1 ? 256 : 1];
+    __shared__ float2 lst[G > 1 ? 256 : 1];
+    const int rows = c.n * c.group, t = threadIdx.x, x = t % W, g = t / W % G;
+    const int64_t total = (int64_t)c.batch * c.kv_heads * rows, at = (int64_t)blockIdx.x * R + t / (W * G);
+    const bool there = t < W * G * R && at < total;
+    float top = -INFINITY, sum = 0.0f;   // the largest score of all, and the sum below it
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](float mx, float ref, float s, f32x4 v) {   // the split's largest score, what it was taken below, its sums
+        if (ref == -INFINITY) return;   // no key of this split
+        const float next = fmaxf(top, mx), f = __builtin_amdgcn_exp2f((top - next) * kLog2eF), h = __builtin_amdgcn_exp2f((ref - next) * kLog2eF);
+        top = next;
+        sum = fmaf(sum, f, s * h);
 #pragma unroll
-        for (int i = 0; i < (DP + 63) / 64; ++i)
-            if (lane + 64 * i < DP) acc[i] = fmaf(c.part[(s * total + at) * DP + lane + 64 * i], f, acc[i]);
+        for (int j = 0; j < 4; ++j) acc[j] = fmaf(acc[j], f, v[j] * h);
+    };
+    if (there)
+        for (int s0 = g; s0 < c.splits; s0 += 4 * G) {
+            f32x4 st[4], v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t slot = min(s0 + k * G, c.splits - 1) * total + at;
+                st[k] = *(const f32x4 *)(c.part_stat + slot * 4);
+                v[k] = *(const f32x4 *)(c.part + slot * DP + 4 * x);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * G < c.splits) add(st[k][0], st[k][1], st[k][2], v[k]);
+        }
+    if constexpr (G > 1) {
+        lacc[t] = acc;
+        lst[t] = make_float2(top, sum);
+        __syncthreads();
+        if (g != 0) return;
+        for (int k = 1; k < G; ++k) add(lst[t + k * W].x, lst[t + k * W].x, lst[t + k * W].y, lacc[t + k * W]);
     }
+    if (!there) return;
     const int64_t bh = at / rows;
     const Packed pk = unpack((int)(at - bh * rows), c.group);
     const int hk = (int)(bh % c.kv_heads), b = (int)(bh / c.kv_heads);
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     T *out = (T *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + (hk * c.group + pk.g) * c.so.head;
 #pragma unroll
-    for (int i = 0; i < (DP + 63) / 64; ++i)
-        if (lane + 64 * i < c.d) out[lane + 64 * i] = (T)(acc[i] * inv);
-    if (lane == 0) *(float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q)) = make_float2(top, sum);
+    for (int j = 0; j < 4; ++j)
+        if (4 * x + j < c.d) out[4 * x + j] = (T)(acc[j] * inv);
+    if (x == 0) *(float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q)) = make_float2(top, sum);
+}
+
+template <typename T, int DP> void join(Ctx *c, const AttnCall &a)
+{
+    const int64_t total = (int64_t)a.batch * a.kv_heads * a.n * a.group;
+    constexpr int W = DP / 4;
+    if (a.splits > 16) k_attn_join<T, DP, 8><<<(unsigned)ceil_div(total, 256 / (8 * W)), 256, 0, c->stream>>>(a);
+    else if (a.splits > 4) k_attn_join<T, DP, 4><<<(unsigned)ceil_div(total, 256 / (4 * W)), 256, 0, c->stream>>>(a);
+    else k_attn_join<T, DP, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
 }
 
 template <typename T, int DP, int KT, int WAVES>
@@ -283,10 +314,7 @@ fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
         else if (load == kVec) k_attn<T, DP, KT, WAVES, false, kVec><<<g, nt, 0, c->stream>>>(a);
         else k_attn<T, DP, KT, WAVES, false, kAny><<<g, nt, 0, c->stream>>>(a);
     }
-    if (a.splits > 1) {
-        const int64_t total = (int64_t)a.batch * a.kv_heads * a.n * a.group;
-        k_attn_join<T, DP><<<(unsigned)ceil_div(total, 4), 256, 0, c->stream>>>(a);
-    }
+    if (a.splits > 1) join<T, DP>(c, a);
     FS_HIP(c, hipGetLastError());
     return FS_OK;
 }

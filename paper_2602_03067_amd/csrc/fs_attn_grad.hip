@@ -426,29 +426,61 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
     }
 }
 
-// Sums over the splits: a wave takes a row of dq (KV: of dk and dv), in the order of the splits.
-template <typename T, int DP, bool KV>
+// Sums over the splits, in an order that does not depend on anything else: of dq, or (KV) of dk and dv.  A thread takes four coordinates of a
+// row and every G-th split, four splits' loads at a time; G groups of threads share a row and meet in LDS.
+template <typename T, int DP, bool KV, int G>
 __global__ __launch_bounds__(256) void k_attn_grad_join(const AttnCall c)
 {
-    const int lane = threadIdx.x & 63, rows = KV ? c.m : c.n * c.group;
-    const int64_t total = (int64_t)c.batch * c.kv_heads * rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= total) return;
-    constexpr int W = KV ? 2 * DP : DP;
-    const int64_t bh = at / rows;
-    const int hk = (int)(bh % c.kv_heads), b = (int)(bh / c.kv_heads), r = (int)(at - bh * rows);
-    for (int col = lane; col < W; col += 64) {
-        float acc = 0.0f;
-        for (int s = 0; s < c.splits; ++s) acc += c.part[(s * total + at) * W + col];
-        const int e = col % DP;
-        if (e >= c.d) continue;
-        if constexpr (KV) {
-            if (col < DP) ((T *)c.dk)[b * c.sdk.batch + (int64_t)r * c.sdk.row + hk * c.sdk.head + e] = (T)(acc * c.scale);
-            else ((T *)c.dv)[b * c.sdv.batch + (int64_t)r * c.sdv.row + hk * c.sdv.head + e] = (T)acc;
-        } else {
-            const Packed pk = unpack(r, c.group);
-            ((T *)c.dq)[b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + (hk * c.group + pk.g) * c.sdq.head + e] = (T)(acc * c.scale);
+    constexpr int W = DP / 4, R = 256 / (W * G);
+    __shared__ f32x4 lacc[G > 1 ? 256 : 1];
+    const int t = threadIdx.x, x = t % W, g = t / W % G, rows = KV ? c.m : c.n * c.group;
+    // (dk and dv of a key are two rows)
+    const int64_t total = (int64_t)c.batch * c.kv_heads * rows * (KV ? 2 : 1), at = (int64_t)blockIdx.x * R + t / (W * G);
+    const bool there = t < W * G * R && at < total;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (there)
+        for (int s0 = g; s0 < c.splits; s0 += 4 * G) {
+            f32x4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = *(const f32x4 *)(c.part + (min(s0 + k * G, c.splits - 1) * total + at) * DP + 4 * x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (s0 + k * G < c.splits) acc += v[k];
         }
+    if constexpr (G > 1) {
+        lacc[t] = acc;
+        __syncthreads();
+        if (g != 0) return;
+        for (int k = 1; k < G; ++k) acc += lacc[t + k * W];
     }
+    if (!there) return;
+    const int64_t row = KV ? at / 2 : at, bh = row / rows;
+    const int hk = (int)(bh % c.kv_heads), b = (int)(bh / c.kv_heads), r = (int)(row - bh * rows);
+    T *out;
+    float f = c.scale;
+    if constexpr (KV) {
+        if (at % 2 == 0) {
+            out = (T *)c.dk + b * c.sdk.batch + (int64_t)r * c.sdk.row + hk * c.sdk.head;
+        } else {
+            out = (T *)c.dv + b * c.sdv.batch + (int64_t)r * c.sdv.row + hk * c.sdv.head;
+            f = 1.0f;
+        }
+    } else {
+        const Packed pk = unpack(r, c.group);
+        out = (T *)c.dq + b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + (hk * c.group + pk.g) * c.sdq.head;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (4 * x + j < c.d) out[4 * x + j] = (T)(acc[j] * f);
+}
+
+template <typename T, int DP, bool KV> void join(Ctx *c, const AttnCall &a)
+{
+    const int64_t total = (int64_t)a.batch * a.kv_heads * (KV ? 2 * (int64_t)a.m : (int64_t)a.n * a.group);
+    constexpr int W = DP / 4;
+    if (a.splits > 16) k_attn_grad_join<T, DP, KV, 8><<<(unsigned)ceil_div(total, 256 / (8 * W)), 256, 0, c->stream>>>(a);
+    else if (a.splits > 4) k_attn_grad_join<T, DP, KV, 4><<<(unsigned)ceil_div(total, 256 / (4 * W)), 256, 0, c->stream>>>(a);
+    else k_attn_grad_join<T, DP, KV, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
 }
 
 template <typename T> __global__ __launch_bounds__(256) void k_attn_dbias(const AttnCall c)
@@ -470,7 +502,6 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
     a.row_stat = (float *)(ws + A.take(p.stat_bytes));
     float *dq_part = (float *)(ws + A.take(p.dq_bytes)), *dkv_part = (float *)(ws + A.take(p.dkv_bytes));
     a.dbias_part = (float *)(ws + A.take(p.dbias_bytes));
-    const int64_t heads = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.n * a.group;
     a.splits = p.q_splits;
     a.part = dq_part;
     if (p.q_grid) {
@@ -483,7 +514,7 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
             else if (keys == kVec) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dq<T, DP, KT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
-        if (a.splits > 1) k_attn_grad_join<T, DP, false><<<(unsigned)ceil_div(heads * rows, 4), 256, 0, c->stream>>>(a);
+        if (a.splits > 1) join<T, DP, false>(c, a);
     }
     a.splits = p.k_splits;
     a.part = dkv_part;
@@ -498,7 +529,7 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
             else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dkv<T, DP, RT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
-        if (a.splits > 1) k_attn_grad_join<T, DP, true><<<(unsigned)ceil_div(heads * a.m, 4), 256, 0, c->stream>>>(a);
+        if (a.splits > 1) join<T, DP, true>(c, a);
         if (a.dbias) k_attn_dbias<T><<<(unsigned)ceil_div((int64_t)a.batch * a.m, 256), 256, 0, c->stream>>>(a);
     }
     FS_HIP(c, hipGetLastError());

@@ -401,8 +401,14 @@ fs_status dispatch(Ctx *c, const NormCall &a, int32_t dtype, int32_t wtype, bool
 
 }  // namespace
 
-// Workgroups of a backward pass: four per CU, or what the rows fill.
-int norm_grad_blocks(const Ctx *c, int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(rows, 4 * (int64_t)c->num_cu)); }
+// Workgroups of a backward pass: four per CU, or as many as the rows fill.
+int norm_grad_blocks(const Ctx *c, int64_t rows, int64_t cols, int32_t dtype)
+{
+    // (rows that a workgroup holds side by side, with 16-byte loads; where these cannot be used it holds no more)
+    const int tpr = threads_per_row(cols, dtype == FS_BF16 ? 8 : 4);
+    const int64_t fill = ceil_div(rows, tpr && tpr < kNormThreads ? kNormThreads / tpr : 1);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(fill, 4 * (int64_t)c->num_cu));
+}
 
 fs_status launch_norm(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, const void *beta,
                       int32_t wtype, float eps, void *y, int64_t ldy, float *stat)
@@ -438,7 +444,7 @@ fs_status launch_norm_grad(Ctx *c, const void *x, int32_t dtype, int64_t rows, i
     a.ldx = ldx;
     a.lddy = lddy;
     a.lddx = lddx;
-    a.blocks = norm_grad_blocks(c, rows);
+    a.blocks = norm_grad_blocks(c, rows, cols, dtype);
     dispatch(c, a, dtype, wtype, true);
     if (a.part) k_norm_wsum<<<(unsigned)ceil_div(2 * cols, 16), 1024, 0, c->stream>>>(part, cols, a.blocks, dgamma, dbeta);
     FS_HIP(c, hipGetLastError());
