@@ -8,6 +8,7 @@ missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional, Tuple
 
@@ -144,6 +145,7 @@ def _dev_f32(t: torch.Tensor, name: str, shape=None):
     return t
 
 
+_get_dtype, _get_is_cuda = operator.attrgetter("dtype"), operator.attrgetter("is_cuda")
 _DTYPES = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
 
 
@@ -438,8 +440,7 @@ class Context:
         ``scale`` defaults to d^-1/2, ``bias`` (sets, keys) is added to the scores (log-weights; -inf removes a key), ``q_len``,
         ``k_len`` are the lengths of padded sets.  ``stat`` is what ``fs_attention_grad`` takes up."""
         a = _attn(q, k, v, scale, causal, q_len, k_len, bias)
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        stat = torch.empty(a.batch, a.q_heads, a.q_rows, 2, dtype=torch.float32, device=q.device)
+        o, stat = q.new_empty(q.shape), q.new_empty((a.batch, a.q_heads, a.q_rows, 2), dtype=torch.float32)
         self._check(self.lib.fs_attention(self.h, ctypes.byref(a), ctypes.byref(_heads(o, "o", q.shape, q.dtype)), stat.data_ptr()),
                     "fs_attention")
         return o, stat
@@ -453,8 +454,8 @@ class Context:
         _dev_f32(stat, "stat", (a.batch, a.q_heads, a.q_rows, 2))
         if want_bias and bias is None:
             raise ValueError("want_bias without a bias")
-        g = [torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v)]
-        db = torch.empty(bias.shape, dtype=q.dtype, device=q.device) if want_bias else None
+        g = [q.new_empty(t.shape) for t in (q, k, v)]
+        db = q.new_empty(bias.shape) if want_bias else None
         h = [ctypes.byref(_heads(t, nm, s, q.dtype)) for t, nm, s in
              ((o, "o", q.shape), (do, "do", q.shape), (g[0], "dq", q.shape), (g[1], "dk", k.shape), (g[2], "dv", k.shape))]
         self._check(self.lib.fs_attention_grad(self.h, ctypes.byref(a), h[0], stat.data_ptr(), h[1], h[2], h[3], h[4],
@@ -469,8 +470,7 @@ class Context:
         if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
             raise TypeError("gamma and beta must have one type")
         wt = _DTYPES[gamma.dtype if gamma is not None else beta.dtype if beta is not None else torch.float32]
-        y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-        stat = torch.empty(rows, 2, dtype=torch.float32, device=x.device)
+        y, stat = x.new_empty((rows, cols)), x.new_empty((rows, 2), dtype=torch.float32)
         self._check(self.lib.fs_layer_norm(self.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), w[0], w[1], wt, eps, y.data_ptr(), cols,
                                            stat.data_ptr()), "fs_layer_norm")
         return y, stat
@@ -484,13 +484,12 @@ class Context:
             raise ValueError("dy must have the shape and type of x")
         _dev_f32(stat, "stat", (rows, 2))
         g = _weights(gamma, "gamma", cols)
-        dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-        dw = torch.empty(2, cols, dtype=torch.float32, device=x.device)
+        dx, dw = x.new_empty((rows, cols)), x.new_empty((2, cols), dtype=torch.float32)
         at = dw.data_ptr()
         self._check(self.lib.fs_layer_norm_grad(self.h, x.data_ptr(), _DTYPES[x.dtype], rows, cols, _ld(x), g,
                                                 FS_F32 if gamma is None else _DTYPES[gamma.dtype], stat.data_ptr(), dy.data_ptr(), _ld(dy),
                                                 dx.data_ptr(), cols, at, at + 4 * cols), "fs_layer_norm_grad")
-        return dx, dw[0], dw[1]
+        return (dx, *dw.unbind(0))
 
     def fs_points_keep(self, prob: Problem) -> None:
         """Declare the clouds of `prob` unchanged until fs_points_release: later calls reuse their derived copies."""
@@ -578,10 +577,11 @@ class AdamW:
         kind = grads[0].dtype
         if kind not in _DTYPES:
             raise TypeError("gradients must be float32 or bfloat16")
-        for g, n in zip(grads, self._sizes):
-            if g.numel() != n or g.dtype is not kind or not g.is_cuda or not g.is_contiguous():
-                raise TypeError("a gradient does not fit its weights")
-        self._at[:, 1] = [g.data_ptr() for g in grads]
+        # (whole lists at a time: with many small tensors these checks are what a step costs)
+        if (list(map(torch.Tensor.numel, grads)) != self._sizes or set(map(_get_dtype, grads)) != {kind} or not all(map(_get_is_cuda, grads))
+                or not all(map(torch.Tensor.is_contiguous, grads))):
+            raise TypeError("a gradient does not fit its weights")
+        self._at[:, 1] = list(map(torch.Tensor.data_ptr, grads))
         a = self._args
         a.lr, (a.beta1, a.beta2), a.eps, a.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
         a.step, a.g_dtype = self.step_count + 1, _DTYPES[kind]

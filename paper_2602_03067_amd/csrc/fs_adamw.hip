@@ -16,7 +16,7 @@ namespace fs {
 namespace {
 
 constexpr int kAdamBlock = 256;     // weights under one scale; 64 lanes, four each
-constexpr int kAdamChunk = 4096;    // weights of a workgroup: four waves, four blocks each
+constexpr int kAdamChunk = 1024;    // weights of a workgroup: four waves, a block each
 constexpr int kTableBytes = 3840;   // of a launch's 4 KB of arguments
 
 enum { kP, kG, kM, kV, kMaster, kMs, kVs, kSlots };
@@ -46,7 +46,7 @@ template <typename T, int N, bool ALN> __device__ inline void load_n(const T *p,
 {
     if constexpr (ALN) {
         typedef T V __attribute__((ext_vector_type(N)));
-        const V u = *(const V *)p;
+        const V u = __builtin_nontemporal_load((const V *)p);
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = (float)u[j];
     } else {
@@ -61,7 +61,7 @@ template <typename T, int N, bool ALN> __device__ inline void store_n(T *p, int6
         V u;
 #pragma unroll
         for (int j = 0; j < N; ++j) u[j] = (T)v[j];
-        *(V *)p = u;
+        __builtin_nontemporal_store(u, (V *)p);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
@@ -70,7 +70,7 @@ template <typename T, int N, bool ALN> __device__ inline void store_n(T *p, int6
 }
 template <bool ALN> __device__ inline uint32_t load_codes(const uint8_t *p, int64_t left)
 {
-    if constexpr (ALN) return *(const uint32_t *)p;
+    if constexpr (ALN) return __builtin_nontemporal_load((const uint32_t *)p);
     uint32_t w = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) w |= (j < left ? (uint32_t)p[j] : 0u) << (8 * j);
@@ -79,7 +79,7 @@ template <bool ALN> __device__ inline uint32_t load_codes(const uint8_t *p, int6
 template <bool ALN> __device__ inline void store_codes(uint8_t *p, int64_t left, uint32_t w)
 {
     if constexpr (ALN) {
-        *(uint32_t *)p = w;
+        __builtin_nontemporal_store(w, (uint32_t *)p);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)

@@ -17,6 +17,8 @@ namespace {
 constexpr int kNormThreads = 256;
 constexpr int kLongThreads = 1024;   // one row per workgroup
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // VEC consecutive elements (VEC > 1: 16 bytes, aligned)
 template <typename T, int VEC> struct Pack {
     T e[VEC];
@@ -27,26 +29,28 @@ template <typename T, int VEC> __device__ inline void load_vec(const T *p, float
         v[0] = (float)p[0];
     } else {
         union {
-            uint4 u;
+            u32x4 u;
             Pack<T, VEC> t;
         } w;
-        w.u = *(const uint4 *)p;
+        w.u = *(const u32x4 *)p;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) v[j] = (float)w.t.e[j];
     }
 }
-template <typename T, int VEC> __device__ inline void store_vec(T *p, const float (&v)[VEC])
+// PAST: past the caches (not a branch on a value: the compiler makes one ordinary store of the two)
+template <typename T, int VEC, bool PAST> __device__ inline void store_vec(T *p, const float (&v)[VEC])
 {
     if constexpr (VEC == 1) {
         p[0] = (T)v[0];
     } else {
         union {
-            uint4 u;
+            u32x4 u;
             Pack<T, VEC> t;
         } w;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) w.t.e[j] = (T)v[j];
-        *(uint4 *)p = w.u;
+        if constexpr (PAST) __builtin_nontemporal_store(w.u, (u32x4 *)p);
+        else *(u32x4 *)p = w.u;
     }
 }
 // (VEC > 1: w is 16-byte aligned, and col a multiple of VEC)
@@ -63,11 +67,27 @@ template <typename W, int VEC> __device__ inline void load_weights(const W *w, i
     }
 }
 
+// v + another lane's v: row_shr by 1, 2, 4, 8 (0x111 ..), the last lane of a row of 16 to the next (0x142) or of 32 to the other half (0x143)
+template <int CTRL, int ROWS> __device__ inline float add_from(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+
 // Sum over the TPR threads of a row; every one of them gets it.
 template <int TPR> __device__ inline float row_sum(float v, float *lds)
 {
+    if constexpr (TPR < 64) {
 #pragma unroll
-    for (int m = 1; m < (TPR < 64 ? TPR : 64); m *= 2) v += __shfl_xor(v, m);
+        for (int m = 1; m < TPR; m *= 2) v += __shfl_xor(v, m);
+    } else {   // within rows of 16 lanes, then across them: the last lane has it all
+        v = add_from<0x111, 0xf>(v);
+        v = add_from<0x112, 0xf>(v);
+        v = add_from<0x114, 0xf>(v);
+        v = add_from<0x118, 0xf>(v);
+        v = add_from<0x142, 0xa>(v);
+        v = add_from<0x143, 0xc>(v);
+        v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    }
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         __syncthreads();   // (what was read from lds before)
@@ -91,9 +111,10 @@ struct NormCall {
     int64_t rows, cols, ldx, ldy, lddy, lddx;
     float eps;
     int32_t blocks;
+    bool past;                  // outputs that no cache will hold until they are read go past them
 };
 
-template <typename T, typename W, int VEC, int NV, int TPR>
+template <typename T, typename W, int VEC, int NV, int TPR, bool PAST>
 __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_norm(const NormCall c)
 {
     constexpr int NT = TPR > kNormThreads ? TPR : kNormThreads, RPB = NT / TPR;
@@ -139,18 +160,19 @@ __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_nor
             load_weights<W, VEC>((const W *)c.beta, col, 0.0f, b);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) v[i][j] = fmaf((v[i][j] - rest) * rstd, g[j], b[j]);
-            store_vec<T, VEC>(y + col, v[i]);
+            store_vec<T, VEC, PAST>(y + col, v[i]);
         }
     }
     if (t == 0 && c.stat) *(float2 *)(c.stat + 2 * row) = make_float2(mean + rest, rstd);
 }
 
-template <typename T, typename W, int VEC, int NV, int TPR>
+template <typename T, typename W, int VEC, int NV, int TPR, bool PAST>
 __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_norm_grad(const NormCall c)
 {
     constexpr int NT = TPR > kNormThreads ? TPR : kNormThreads, RPB = NT / TPR;
     __shared__ float lds[3][TPR > 64 ? TPR / 64 : 1];
-    __shared__ float lsum[RPB > 1 ? RPB * TPR * VEC : 1];
+    constexpr int SIDE = TPR < 64 ? NT / 64 : RPB, WIDE = TPR < 64 ? 64 : TPR;   // waves, or rows, side by side
+    __shared__ float lsum[SIDE > 1 ? SIDE * TPR * VEC : 1];
     const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     float g[NV][VEC], dg[NV][VEC], db[NV][VEC];
 #pragma unroll
@@ -207,7 +229,7 @@ __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_nor
                     db[i][j] += w[i][j];
                     w[i][j] = st.y * (fmaf(w[i][j], g[i][j], -s1) - v[i][j] * s2);
                 }
-                if (live && c.dx) store_vec<T, VEC>(dx + col, w[i]);
+                if (live && c.dx) store_vec<T, VEC, PAST>(dx + col, w[i]);
             }
         }
     }
@@ -222,16 +244,27 @@ __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_nor
             float a[VEC];
 #pragma unroll
             for (int j = 0; j < VEC; ++j) a[j] = k ? db[i][j] : dg[i][j];
-            if constexpr (RPB > 1) {
-                __syncthreads();
+            if constexpr (TPR < 64) {   // rows of one wave
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) lsum[(slot * VEC + j) * TPR + t] = a[j];
-                __syncthreads();
+                for (int m = TPR; m < 64; m *= 2)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    a[j] = 0.0f;
-                    if (slot == 0)
-                        for (int q = 0; q < RPB; ++q) a[j] += lsum[(q * VEC + j) * TPR + t];
+                    for (int j = 0; j < VEC; ++j) a[j] += __shfl_xor(a[j], m);
+            }
+            if constexpr (SIDE > 1) {
+                const int side = threadIdx.x / WIDE;
+                __syncthreads();
+                if (threadIdx.x % WIDE < TPR) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) lsum[(side * VEC + j) * TPR + t] = a[j];
+                }
+                __syncthreads();
+                if (slot == 0) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        a[j] = 0.0f;
+#pragma unroll
+                        for (int q = 0; q < SIDE; ++q) a[j] += lsum[(q * VEC + j) * TPR + t];
+                    }
                 }
             }
             if (slot == 0 && col < c.cols) {
@@ -321,6 +354,7 @@ __global__ __launch_bounds__(1024) void k_norm_wsum(const float *part, int64_t c
     const int lane = threadIdx.x / 16;
     float s = 0.0f;
     if (col < wide)
+#pragma unroll 4
         for (int b = lane; b < blocks; b += 64) s += part[b * wide + col];
     lds[lane][threadIdx.x % 16] = s;
     __syncthreads();
@@ -347,8 +381,14 @@ int threads_per_row(int64_t cols, int vec)
 template <typename T, typename W, int VEC, int NV, int TPR> fs_status run(Ctx *c, const NormCall &a, bool grad)
 {
     constexpr int NT = TPR > kNormThreads ? TPR : kNormThreads;
-    if (grad) k_norm_grad<T, W, VEC, NV, TPR><<<(unsigned)a.blocks, NT, 0, c->stream>>>(a);
-    else k_norm<T, W, VEC, NV, TPR><<<(unsigned)ceil_div(a.rows, NT / TPR), NT, 0, c->stream>>>(a);
+    const unsigned grid = (unsigned)(grad ? a.blocks : ceil_div(a.rows, NT / TPR));
+    if (VEC > 1 && a.past) {
+        if (grad) k_norm_grad<T, W, VEC, NV, TPR, (VEC > 1)><<<grid, NT, 0, c->stream>>>(a);
+        else k_norm<T, W, VEC, NV, TPR, (VEC > 1)><<<grid, NT, 0, c->stream>>>(a);
+    } else {
+        if (grad) k_norm_grad<T, W, VEC, NV, TPR, false><<<grid, NT, 0, c->stream>>>(a);
+        else k_norm<T, W, VEC, NV, TPR, false><<<grid, NT, 0, c->stream>>>(a);
+    }
     return FS_OK;
 }
 
@@ -393,8 +433,11 @@ template <typename T, typename W> fs_status by_alignment(Ctx *c, const NormCall 
     return vec ? by_length<T, W, V>(c, a, grad) : by_length<T, W, 1>(c, a, grad);
 }
 
-fs_status dispatch(Ctx *c, const NormCall &a, int32_t dtype, int32_t wtype, bool grad)
+fs_status dispatch(Ctx *c, NormCall a, int32_t dtype, int32_t wtype, bool grad)
 {
+    // An output beyond the 4 MB of L2 of eight XCDs (forward and backward, with and without, us: 70000 x 784 float 205 and 224,
+    // 50000 x 1024 bf16 104 and 105; loads past the caches as well: 205 and 106)
+    a.past = a.rows * a.cols * (dtype == FS_BF16 ? 2 : 4) > (int64_t(32) << 20);
     if (dtype == FS_F32) return wtype == FS_F32 ? by_alignment<float, float>(c, a, grad) : by_alignment<float, __bf16>(c, a, grad);
     return wtype == FS_F32 ? by_alignment<__bf16, float>(c, a, grad) : by_alignment<__bf16, __bf16>(c, a, grad);
 }
