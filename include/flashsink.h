@@ -394,7 +394,9 @@ fs_status fs_points_release(fs_ctx *ctx);
  * kv_heads divides q_heads; head h reads keys and values of head h / (q_heads / kv_heads).  d <= 128 coordinates.
  * Lengths may be 0 and 1, strides are in elements, any alignment will do (rows of whole 16 bytes, aligned to them, are
  * read fastest).
- * FS_F32: products on the fp32 matrix cores.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
+ * FS_F32: products on the fp32 matrix cores; where that takes long enough (1.5e9 operations, the backward pass counted 2.5 times),
+ * from operands in two fp16 pieces, 22 bits of every element down to 2^-17 of its head's largest and 2^-40 of that below, summed in
+ * fp32.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
  * probabilities (2^-9 of each) and their gradients are rounded to bf16 where they enter a second product.  Maxima, sums
  * and accumulators are fp32 in both.
  */
@@ -492,6 +494,7 @@ fs_status fs_adamw(fs_ctx *ctx, const fs_adamw_args *args /* host */, const fs_a
  *   "fx_long"            1: fixed-point half-steps of any length as long ones, which leave tiles that cannot count early, 2: none
  *   "fx_count"           1: count the tiles of long fixed-point half-steps from zero (16 bytes of device memory; kernels of their
  *                        own, slower ones), 0: don't.  Synchronises the stream.
+ *   "attn_pairs"         1: float32 attention through pairs of fp16 at any size, 2: never
  * Unknown keys and values out of range: FS_ERR_INVALID_ARG.  key: HOST string.
  */
 fs_status fs_debug_set(fs_ctx *ctx, const char *key /* host */, int64_t value);

@@ -1432,12 +1432,13 @@ fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, floa
     const bool f32 = attn->dtype == FS_F32;
     const AttnPlan p = attn_plan(c, a, f32);
     a.splits = p.splits;
-    if (p.splits > 1) {
+    if (p.splits > 1 || p.pairs) {
         Arena A;
-        const size_t part = A.take(p.part_bytes), ps = A.take(p.stat_bytes);
+        const size_t part = A.take(p.part_bytes), ps = A.take(p.stat_bytes), pairs = A.take(p.pair_bytes);
         if ((st = ensure_aux(c, A.off))) return st;
         a.part = (float *)(c->aux + part);
         a.part_stat = (float *)(c->aux + ps);
+        if (p.pairs) pair_layout(&a, c->aux + pairs, false);
     }
     return launch_attn(c, a, p, f32, k.aligned);
 }
@@ -1492,7 +1493,9 @@ fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o,
     A.take(p.dq_bytes);
     A.take(p.dkv_bytes);
     A.take(p.dbias_bytes);
+    const size_t pairs = A.take(p.pair_bytes);
     if ((st = ensure_aux(c, A.off))) return st;
+    if (p.pairs) pair_layout(&a, c->aux + pairs, true);
     return launch_attn_grad(c, a, p, c->aux, f32, k.aligned);
 }
 
@@ -1628,6 +1631,8 @@ fs_status fs_debug_set(fs_ctx *ctx, const char *key, int64_t value)
         c->dbg_fx_splits = (int)value;
     else if (k == "moment_kind" && value >= 0 && value <= 7)
         c->dbg_moment_kind = (int)value;
+    else if (k == "attn_pairs" && value >= 0 && value <= 2)
+        c->dbg_attn_pairs = (int)value;
     else if (k == "fx_long" && value >= 0 && value <= 2)
         c->dbg_fx_long = (int)value;
     else if (k == "fx_count" && (value == 0 || value == 1)) {

@@ -1,12 +1,14 @@
 // What the forward and the backward kernels of attention share: operands of the matrix cores, tiles in LDS, and the
 // description of a call.
 //
-// Both element types go through 32 x 32 products whose operands are 16 bytes a lane: eight bf16 (one v_mfma_f32_32x32x16_bf16)
+// Element types go through 32 x 32 products whose operands are 16 bytes a lane: eight bf16 (one v_mfma_f32_32x32x16_bf16)
 // or four floats (four v_mfma_f32_32x32x2_f32).  Lane l = 32 h + c holds row (column) c of the operand and the contraction
 // indices kStep t + (kStep / 2) h + 0, 1, ..; register r of a product holds row 8 (r / 4) + 4 h + r % 4 of column c.  So the
 // registers of one product, a step's share at a time, are the second operand of the next one as they stand, if its first operand
 // takes the rows in that order: probabilities never pass through LDS.
 #pragma once
+
+#include <type_traits>
 
 #include "fs_internal.h"
 
@@ -19,8 +21,50 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 template <typename T> struct Mma;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Floats as the sum of two fp16, under a power of two for all of a head's rows that puts the largest into [2^14, 2^15): 22 bits of
+// every element down to 2^-17 of the largest, and never less than 2^-40 of it.  A product takes three products of the pieces
+// (the two lower ones' is below 2^-22), three v_mfma_f32_32x32x16_f16 of 32 cycles for sixteen coordinates, where the fp32
+// matrix cores take eight of 64.
+struct Pair {};
+template <> struct Mma<Pair> {
+    using Elem = float;
+    struct Frag {
+        f16x8 h, l;
+    };
+    static constexpr int kStep = 16;
+    static constexpr int kPiece = 8;
+    static __device__ inline f32x16 mma(const Frag &a, const Frag &b, f32x16 c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.l, b.h, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.h, b.l, c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.h, b.h, c, 0, 0, 0);
+    }
+    static __device__ inline void split(float v, _Float16 &h, _Float16 &l)
+    {
+        // v as a float first: where a product is converted, one instruction may round it to fp16 at once, which near a tie is not the
+        // upper piece that the lower one was taken off
+        asm volatile("" : "+v"(v));
+        h = (_Float16)v;
+        l = (_Float16)(v - (float)h);
+    }
+    static __device__ inline Frag pack(const f32x16 &v, int t)
+    {
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            _Float16 h, l;
+            split(v[8 * t + j], h, l);
+            f.h[j] = h;
+            f.l[j] = l;
+        }
+        return f;
+    }
+};
 
 template <> struct Mma<__bf16> {
+    using Elem = __bf16;
     using Frag = bf16x8;
     static constexpr int kStep = 16;    // contraction indices of a fragment
     static constexpr int kPiece = 8;    // elements of 16 bytes
@@ -33,10 +77,10 @@ template <> struct Mma<__bf16> {
         for (int j = 0; j < 8; ++j) f[j] = (__bf16)v[8 * t + j];
         return f;
     }
-    static __device__ inline float load(const __bf16 *p) { return (float)*p; }
 };
 
 template <> struct Mma<float> {
+    using Elem = float;
     using Frag = f32x4;
     static constexpr int kStep = 8;
     static constexpr int kPiece = 4;
@@ -53,7 +97,6 @@ template <> struct Mma<float> {
         for (int j = 0; j < 4; ++j) f[j] = v[4 * t + j];
         return f;
     }
-    static __device__ inline float load(const float *p) { return *p; }
 };
 
 // A tile of rows in LDS, DP elements each (zero beyond d).  16-byte pieces are permuted within their row so that the lanes of a
@@ -114,6 +157,42 @@ template <typename T, int DP> struct Tile {
         }
     }
 };
+// Pairs: 32 rows of the upper pieces, then of the lower, each like a bf16 tile.
+template <int DP> struct Tile<Pair, DP> {
+    using B = Tile<__bf16, DP>;
+    using Lanes = typename B::Lanes;
+    using Frag = Mma<Pair>::Frag;
+    static constexpr int kRow = 2 * B::kRow, kPieces = 2 * B::kPieces;
+    static constexpr int kSub = 32 * kRow, kLower = 32 * B::kRow;
+    static __device__ inline Lanes lanes(int lane) { return B::lanes(lane); }
+    static __device__ inline Frag rows(LdsPtr lds, const Lanes &b, int row0, int t)
+    {
+        const LdsPtr p = lds + row0 / 32 * kSub;
+        return {__builtin_bit_cast(f16x8, B::rows(p, b, 0, t)), __builtin_bit_cast(f16x8, B::rows(p + kLower, b, 0, t))};
+    }
+    static __device__ inline Frag cols(LdsPtr lds, const Lanes &b, int row0, int t, int db, int lane)
+    {
+        const LdsPtr p = lds + row0 / 32 * kSub;
+        return {__builtin_bit_cast(f16x8, B::cols(p, b, 0, t, db, lane)), __builtin_bit_cast(f16x8, B::cols(p + kLower, b, 0, t, db, lane))};
+    }
+    // a lane's operand from an image (see PairImage): step t of row `row`
+    static __device__ inline Frag from_image(const char *img, int row, int t, int half)
+    {
+        const char *p = img + (int64_t)(row >> 5) * kSub + B::at(row & 31, 2 * t + half);
+        return {*(const f16x8 *)p, *(const f16x8 *)(p + kLower)};
+    }
+};
+// tiles of an image lie in memory as in LDS: linear copies
+template <int DP, int ROWS, int NT> struct DmaImage {
+    static constexpr int kTile = ROWS * Tile<Pair, DP>::kRow, kCount = kTile / 16 / NT;
+    static_assert(kTile % (16 * NT) == 0, "");
+    static __device__ inline void load(const char *tile, unsigned lds, int tid)
+    {
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds + (tid >> 6) * 1024);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) dma16s(tile + i * NT * 16, tid * 16, to + i * NT * 16);
+    }
+};
 __device__ inline unsigned lds_address(LdsPtr p) { return (unsigned)(uintptr_t)p; }
 
 // How a tile comes to LDS.
@@ -122,6 +201,7 @@ __device__ inline unsigned lds_address(LdsPtr p) { return (unsigned)(uintptr_t)p
 //  kVec   through registers, 16 bytes a load: aligned rows
 //  kAny   through registers, an element a load
 // The registers' way can leave out what removed keys (bias of minus infinity) hold; the direct one reads whole tiles.
+// (Pairs are always direct; there the two others say how rows of the tensors themselves are read.)
 enum Load { kDma, kVec, kAny };
 
 // Direct loads of a tile of ROWS rows by NT threads: LDS takes consecutive 16-byte pieces of consecutive lanes, so a lane fetches the piece
@@ -206,7 +286,21 @@ struct HeadsAt {
     int64_t batch, row, head;
 };
 
+// Pairs of a call in the workspace: per (set, kv head) tiles of 32 packed rows (or keys), padded to 128 rows, zero where nothing is
+// admitted; and eight floats: the scales of q, k, v and do (powers of two) and the largest row norms of v and do.
+enum { kPairQ, kPairK, kPairV, kPairDo, kPairTensors };
+struct PairImage {
+    char *img[kPairTensors];
+    float *scale;
+    float *part;   // maxima of chunks of rows
+};
+constexpr float kPairP = 16.0f;      // probabilities below a reference enter the second product times this (up to 2^11: attn_slack)
+constexpr float kPairN = 32768.0f;   // normalised ones times this
+
+__host__ __device__ inline int64_t pair_rows(int64_t rows) { return (rows + 127) / 128 * 128; }
+
 struct AttnCall {
+    PairImage pair;
     const void *q, *k, *v;
     HeadsAt sq, sk, sv;
     void *o;                     // forward: written; backward: read
@@ -270,11 +364,18 @@ __device__ inline Work work_of(int id, int total, int splits, int blocks, int kv
     return w;
 }
 
+// Whether a float32 call goes through pairs, the bytes that they take (each piece rounded up to 256), and their making.
+bool pair_worth(const Ctx *c, const AttnCall &a, bool grad);
+size_t pair_bytes(const AttnCall &a, bool grad);
+void pair_layout(AttnCall *a, char *ws, bool grad);
+fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad);
+
 // how a forward pass is launched
 struct AttnPlan {
     int waves, splits;
+    bool pairs;
     int64_t grid;
-    size_t part_bytes, stat_bytes;
+    size_t part_bytes, stat_bytes, pair_bytes;
 };
 AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32);
 fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bool aligned);
@@ -282,12 +383,42 @@ fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bo
 // ... and a backward pass: rows' side (dq) and keys' side (dk, dv)
 struct AttnGradPlan {
     int q_splits, k_splits;
+    bool pairs;
     int64_t q_grid, k_grid;
-    size_t stat_bytes, dq_bytes, dkv_bytes, dbias_bytes;
+    size_t stat_bytes, dq_bytes, dkv_bytes, dbias_bytes, pair_bytes;
 };
 AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32);
 // `ws`: the bytes of the plan, each piece rounded up to 256
 fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool f32, bool aligned);
+
+// What turns products of pieces into what they stand for (all powers of two but the first).  The gradient of a score is at most 2 |do| |v|
+// in size: times `ds`, from the largest norms, it is inside fp16.
+struct PairScale {
+    float score;   // of <q, k>, with the call's own scale
+    float v, dov;  // 1 / scale of v, ds / (scales of do and v)
+    float ds;
+    float dq, dk, dv;   // of the sums over ds k, ds q and kPairN p do
+};
+__device__ inline PairScale pair_scale(const AttnCall &c, int64_t bh)
+{
+    const float *s = c.pair.scale + 8 * bh;
+    const float q = 1.0f / s[kPairQ], k = 1.0f / s[kPairK], v = 1.0f / s[kPairV];
+    PairScale p;
+    p.score = c.scale * q * k;
+    p.v = v;
+    p.dov = p.ds = p.dq = p.dk = p.dv = 0.0f;
+    if (c.pair.img[kPairDo]) {
+        const float g = 1.0f / s[kPairDo], n = s[4] * s[5];
+        int e = 127 + 13 - ((int)(__builtin_bit_cast(uint32_t, n) >> 23) - 127);   // n < 2^(e + 1): ds n in (2^12, 2^14]
+        e = e < 1 ? 1 : e > 240 ? 240 : e;
+        p.ds = n == 0.0f ? 1.0f : __builtin_bit_cast(float, (uint32_t)e << 23);
+        p.dov = p.ds * g * v;
+        p.dq = k / p.ds;
+        p.dk = q / p.ds;
+        p.dv = g / kPairN;
+    }
+    return p;
+}
 
 __device__ inline float across_halves_max(float v)
 {

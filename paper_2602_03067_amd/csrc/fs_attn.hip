@@ -16,21 +16,23 @@ constexpr float kLog2eF = 1.44269504088896340736f;
 // second loop, which follows the maximum and rescales in every tile.  (With the rescaling in a branch of one loop the compiler
 // keeps two copies of the accumulators and moves them to and fro.)
 constexpr float kSlack = 30.0f;
+constexpr float kSlackPair = 11.0f;   // (kPairP times a probability is an fp16)
 
 // waves per SIMD: what registers allow without spills
-constexpr int min_waves(size_t elem, int dp) { return elem == 4 && dp >= 96 ? 1 : 2; }
+template <typename T> constexpr int min_waves(int dp) { return std::is_same<T, float>::value && dp >= 96 ? 1 : 2; }
 
 template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD>
-__global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(const AttnCall c)
+__global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const AttnCall c)
 {
     using M = Mma<T>;
+    using E = typename M::Elem;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
     using D = Dma<T, DP, KT, 64 * WAVES>;
-    constexpr bool ALN = LOAD != kAny;
+    constexpr bool ALN = LOAD != kAny, kPair = std::is_same<T, Pair>::value, kDirect = kPair || LOAD == kDma;
     constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
     constexpr int kTile = D::kTile, NPC = D::kCount;
-    static_assert(KT * TL::kPieces % NT == 0, "");
+    static_assert(KT * TL::kPieces % NT == 0 && (!kPair || WAVES == 4), "");
     __shared__ __align__(16) char lds[4 * kTile];
     __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
 
@@ -51,69 +53,81 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
     const int tiles = (hi + KT - 1) / KT, per = (tiles + c.splits - 1) / c.splits;
     const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
 
-    const T *kp = (const T *)c.k + b * c.sk.batch + hk * c.sk.head;
-    const T *vp = (const T *)c.v + b * c.sv.batch + hk * c.sv.head;
+    const E *kp = (const E *)c.k + b * c.sk.batch + hk * c.sk.head;
+    const E *vp = (const E *)c.v + b * c.sv.batch + hk * c.sv.head;
+    const int64_t bh = (int64_t)b * c.kv_heads + hk;
+    PairScale ps;
+    if constexpr (kPair) ps = pair_scale(c, bh);
+    const float scale = kPair ? ps.score : c.scale;
     const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
     const LdsPtr base = (LdsPtr)lds;
 
     // what a thread fetches of a tile
     unsigned ko[D::kOffsets], vo[D::kOffsets];
-    uint4 kr[LOAD == kDma ? 1 : NPC], vr[LOAD == kDma ? 1 : NPC];
+    uint4 kr[kDirect ? 1 : NPC], vr[kDirect ? 1 : NPC];
     float br = 0.0f;
-    if constexpr (LOAD == kDma) {
+    if constexpr (!kPair && LOAD == kDma) {
 #pragma unroll
         for (int i = 0; i < D::kOffsets; ++i) {
-            ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
-            vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+            ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(E) + D::piece(tid, i) * 16);
+            vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(E) + D::piece(tid, i) * 16);
         }
         if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KT, t1 - t0);
     }
     // kDma: the whole way; otherwise to registers
     auto fetch = [&](int tile, int buf) {
-        if constexpr (LOAD == kDma) {
+        if constexpr (kPair) {
+            const int64_t at = (bh * pair_rows(c.m) + (int64_t)tile * KT) * TL::kRow;
+            const unsigned to = lds_address(base) + 2 * buf * kTile;
+            DmaImage<DP, KT, NT>::load(c.pair.img[kPairK] + at, to, tid);
+            DmaImage<DP, KT, NT>::load(c.pair.img[kPairV] + at, to + kTile, tid);
+        } else if constexpr (LOAD == kDma) {
             const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(T), to, tid, c.d, k_len - tile * KT);
-            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(T), to + kTile, tid, c.d, k_len - tile * KT);
+            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(E), to, tid, c.d, k_len - tile * KT);
+            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(E), to + kTile, tid, c.d, k_len - tile * KT);
         } else {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
                 const int p = tid + i * NT, pc = p % TL::kPieces, key = tile * KT + p / TL::kPieces, at = min(key, k_len - 1);
-                kr[i] = load_piece<T, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
-                vr[i] = load_piece<T, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
+                kr[i] = load_piece<E, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
+                vr[i] = load_piece<E, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
                 if (BIAS && bp[at] == -INFINITY) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);   // what removed keys hold does not matter
             }
-            if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
         }
+        if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
     };
     auto put = [&](int buf) {
-        if constexpr (LOAD != kDma) {
+        if constexpr (!kDirect) {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
                 const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
                 *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
                 *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
             }
-            if (BIAS && tid < KT) lbias[buf][tid] = br;
         }
+        if (BIAS && tid < KT) lbias[buf][tid] = br;
     };
 
     if (t0 < t1) fetch(t0, 0);
     Frag q[NS];
-    {
-        const T *row = (const T *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + (hk * c.group + pk.g) * c.sq.head;
+    if constexpr (kPair) {
+#pragma unroll
+        for (int t = 0; t < NS; ++t) q[t] = TL::from_image(c.pair.img[kPairQ] + bh * pair_rows(rows) * TL::kRow, r, t, half);
+    } else {
+        const E *row = (const E *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + (hk * c.group + pk.g) * c.sq.head;
 #pragma unroll
         for (int t = 0; t < NS; ++t)
-            q[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(row, 2 * t + half, c.d) : make_uint4(0, 0, 0, 0));
+            q[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(row, 2 * t + half, c.d) : make_uint4(0, 0, 0, 0));
     }
     f32x16 o[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) o[i] = (f32x16)(0.0f);
     // units of the running values: without bias the products <q, k>, with it the scores
-    const float unit = BIAS ? kLog2eF : c.scale * kLog2eF;
+    const float unit = BIAS ? kLog2eF : scale * kLog2eF;
     // exp2((s - ref) unit), the difference first: a bias of the type's lowest value times log2 e would leave the type, and full
     // precision is not to lose an ulp of the larger of the two.  In bf16 without bias one fma does.
-    constexpr bool kDiff = BIAS || sizeof(T) == 4;
+    constexpr bool kDiff = BIAS || sizeof(E) == 4;
     float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
     const typename TL::Lanes ln = TL::lanes(lane);
 
@@ -138,7 +152,7 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
                 for (int g = 0; g < 4; ++g) {
                     const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * g + 4 * half];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], c.scale, add[j]);
+                    for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], scale, add[j]);
                 }
         }
         if (__any(limit < (tile + 1) * KT)) {
@@ -165,7 +179,8 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float e = kDiff ? __builtin_amdgcn_exp2f((s[nb][i] - safe) * unit)
+                const float e = kPair ? __builtin_amdgcn_exp2f(fmaf(s[nb][i] - safe, unit, 4.0f))   // kPairP = 2^4
+                              : kDiff ? __builtin_amdgcn_exp2f((s[nb][i] - safe) * unit)
                                       : __builtin_amdgcn_exp2f(fmaf(s[nb][i], unit, -off));
                 s[nb][i] = e;
                 part += e;
@@ -182,8 +197,8 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
             }
     };
     auto next_tile = [&](int tile) {
-        if (LOAD != kDma && tile + 1 < t1) put((tile + 1 - t0) & 1);
-        if (LOAD == kDma) dma_wait();
+        if ((!kDirect || BIAS) && tile + 1 < t1) put((tile + 1 - t0) & 1);
+        if (kDirect) dma_wait();
         __syncthreads();
     };
     int tile = t0;
@@ -193,7 +208,7 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
         f32x16 s[NB];
         const float mx = scores(tile, s);
         ref = ref == -INFINITY ? mx : ref;
-        fetched = __any((mx - ref) * unit > kSlack);
+        fetched = __any((mx - ref) * unit > (kPair ? kSlackPair : kSlack));
         if (fetched) break;
         top = fmaxf(top, mx);
         accumulate(tile, s);
@@ -216,9 +231,14 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
 
     sum = across_halves_sum(sum);
     if (r >= rows) return;
-    const float st = BIAS ? 1.0f : c.scale;   // the running values as scores
+    const float st = BIAS ? 1.0f : scale;   // the running values as scores
+    if constexpr (kPair) {
+        sum /= kPairP;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) o[i] *= ps.v / kPairP;
+    }
     if (c.splits > 1) {
-        const int64_t at = ((int64_t)split * c.batch * c.kv_heads + (int64_t)b * c.kv_heads + hk) * rows + r;
+        const int64_t at = ((int64_t)split * c.batch * c.kv_heads + bh) * rows + r;
         float *po = c.part + at * DP + 4 * half;
 #pragma unroll
         for (int i = 0; i < ND; ++i)
@@ -229,11 +249,11 @@ __global__ __launch_bounds__(64 * WAVES, min_waves(sizeof(T), DP)) void k_attn(c
         return;
     }
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-    T *out = (T *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + (hk * c.group + pk.g) * c.so.head;
+    E *out = (E *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + (hk * c.group + pk.g) * c.so.head;
 #pragma unroll
-    for (int i = 0; i < ND; ++i) store_column<T, ALN>(out, o[i], inv, 32 * i + 4 * half, c.d);
+    for (int i = 0; i < ND; ++i) store_column<E, ALN>(out, o[i], inv, 32 * i + 4 * half, c.d);
     if (half == 0) {
-        const int64_t at = (((int64_t)b * c.kv_heads + hk) * c.group + pk.g) * c.n + pk.q;
+        const int64_t at = (bh * c.group + pk.g) * c.n + pk.q;
         // the sum below the maximum itself
         const float safe = ref == -INFINITY ? 0.0f : ref;
         *(float2 *)(c.stat + 2 * at) = make_float2(top * st, sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f((safe - top) * unit));
@@ -306,7 +326,15 @@ template <typename T, int DP, int KT, int WAVES>
 fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
 {
     const unsigned g = (unsigned)grid, nt = 64 * WAVES;
-    if (a.bias) {
+    if constexpr (std::is_same<T, Pair>::value) {   // (rows of the tensors themselves are only written)
+        if (a.bias) {
+            if (load != kAny) k_attn<T, DP, KT, WAVES, true, kVec><<<g, nt, 0, c->stream>>>(a);
+            else k_attn<T, DP, KT, WAVES, true, kAny><<<g, nt, 0, c->stream>>>(a);
+        } else {
+            if (load != kAny) k_attn<T, DP, KT, WAVES, false, kVec><<<g, nt, 0, c->stream>>>(a);
+            else k_attn<T, DP, KT, WAVES, false, kAny><<<g, nt, 0, c->stream>>>(a);
+        }
+    } else if (a.bias) {
         if (load != kAny) k_attn<T, DP, KT, WAVES, true, kVec><<<g, nt, 0, c->stream>>>(a);
         else k_attn<T, DP, KT, WAVES, true, kAny><<<g, nt, 0, c->stream>>>(a);
     } else {
@@ -314,9 +342,19 @@ fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
         else if (load == kVec) k_attn<T, DP, KT, WAVES, false, kVec><<<g, nt, 0, c->stream>>>(a);
         else k_attn<T, DP, KT, WAVES, false, kAny><<<g, nt, 0, c->stream>>>(a);
     }
-    if (a.splits > 1) join<T, DP>(c, a);
+    if (a.splits > 1) join<typename Mma<T>::Elem, DP>(c, a);
     FS_HIP(c, hipGetLastError());
     return FS_OK;
+}
+
+fs_status pairs_by_width(Ctx *c, const AttnCall &a, Load load, int64_t grid)
+{
+    switch ((a.d + 31) / 32) {
+    case 1: return run<Pair, 32, 64, 4>(c, a, load, grid);
+    case 2: return run<Pair, 64, 64, 4>(c, a, load, grid);
+    case 3: return run<Pair, 96, 32, 4>(c, a, load, grid);
+    default: return run<Pair, 128, 32, 4>(c, a, load, grid);
+    }
 }
 
 template <typename T>
@@ -346,7 +384,8 @@ AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
 {
     AttnPlan p;
     const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads;
-    p.waves = rows <= 32 ? 1 : 4;
+    p.pairs = f32 && pair_worth(c, a, false);
+    p.waves = rows <= 32 && !p.pairs ? 1 : 4;
     const int kt = p.waves == 1 || f32 ? 32 : 64;
     const int64_t blocks = ceil_div(rows, 32 * p.waves) * heads, tiles = ceil_div(a.m, kt);
     const int64_t want = (int64_t)c->num_cu * (p.waves == 1 ? 4 : 2);
@@ -354,6 +393,7 @@ AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
     p.grid = blocks * p.splits;
     const int64_t dp = round_up(a.d, 32), total = heads * rows * p.splits;
     p.part_bytes = p.splits > 1 ? (size_t)total * dp * 4 : 0;
+    p.pair_bytes = p.pairs ? pair_bytes(a, false) : 0;
     p.stat_bytes = p.splits > 1 ? (size_t)total * 16 : 0;
     return p;
 }
@@ -363,6 +403,10 @@ fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bo
     // (offsets of 64 rows in 32 bits)
     const int64_t most = std::max(a.sk.row, a.sv.row) * (f32 ? 4 : 2) * 64;
     const Load load = !aligned ? kAny : most < (int64_t(1) << 31) ? kDma : kVec;
+    if (p.pairs) {
+        const fs_status st = launch_pairs(c, a, false);
+        return st ? st : pairs_by_width(c, a, load, p.grid);
+    }
     return f32 ? by_width<float>(c, a, load, p.waves, p.grid) : by_width<__bf16>(c, a, load, p.waves, p.grid);
 }
 

@@ -27,23 +27,27 @@ template <bool DIFF> __device__ inline RowStat row_stat(float top, float sum)
 
 constexpr int kRowBlock = 128;   // packed rows of a dq workgroup; the row statistics are padded to whole ones
 __device__ inline int64_t round_up_rows(int rows) { return ((int64_t)rows + kRowBlock - 1) / kRowBlock * kRowBlock; }
-constexpr int row_tile(size_t elem) { return elem == 2 ? 64 : 32; }
+template <typename T> constexpr int row_tile(int dp) { return std::is_same<T, __bf16>::value || (std::is_same<T, Pair>::value && dp <= 64) ? 64 : 32; }
 
 // waves per SIMD: what registers allow without spills
-constexpr int dq_waves(size_t elem, int dp) { return elem == 4 && dp >= 96 ? 1 : 2; }
-constexpr int dkv_waves(size_t elem, int dp) { return elem == 4 ? (dp >= 64 ? 1 : 2) : dp >= 160 ? 1 : 2; }
+template <typename T> constexpr int dq_waves(int dp) { return std::is_same<T, __bf16>::value || dp < 96 ? 2 : 1; }
+template <typename T> constexpr int dkv_waves(int dp)
+{
+    return std::is_same<T, __bf16>::value || dp < (std::is_same<T, Pair>::value ? 96 : 64) ? 2 : 1;
+}
 
 template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD>
-__global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq(const AttnCall c)
+__global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const AttnCall c)
 {
     using M = Mma<T>;
+    using E = typename M::Elem;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
     using D = Dma<T, DP, KT, 64 * WAVES>;
-    constexpr bool ALN = LOAD != kAny;
+    constexpr bool ALN = LOAD != kAny, kPair = std::is_same<T, Pair>::value, kDirect = kPair || LOAD == kDma;
     constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
     constexpr int kTile = D::kTile, NPC = D::kCount;
-    constexpr bool kDiff = BIAS || sizeof(T) == 4;
+    constexpr bool kDiff = BIAS || sizeof(E) == 4;
     static_assert(KT * TL::kPieces % NT == 0 && 32 * WAVES == kRowBlock, "");
     __shared__ __align__(16) char lds[4 * kTile];
     __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
@@ -64,72 +68,93 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
     const int tiles = (hi + KT - 1) / KT, per = (tiles + c.splits - 1) / c.splits;
     const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
 
-    const T *kp = (const T *)c.k + b * c.sk.batch + hk * c.sk.head;
-    const T *vp = (const T *)c.v + b * c.sv.batch + hk * c.sv.head;
+    const E *kp = (const E *)c.k + b * c.sk.batch + hk * c.sk.head;
+    const E *vp = (const E *)c.v + b * c.sv.batch + hk * c.sv.head;
+    const int64_t bh = (int64_t)b * c.kv_heads + hk;
+    PairScale ps;
+    if constexpr (kPair) ps = pair_scale(c, bh);
+    const float scale = kPair ? ps.score : c.scale;
     const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
     const LdsPtr base = (LdsPtr)lds;
 
     // (tiles of keys as in k_attn)
     unsigned ko[D::kOffsets], vo[D::kOffsets];
-    uint4 kr[LOAD == kDma ? 1 : NPC], vr[LOAD == kDma ? 1 : NPC];
+    uint4 kr[kDirect ? 1 : NPC], vr[kDirect ? 1 : NPC];
     float br = 0.0f;
-    if constexpr (LOAD == kDma) {
+    if constexpr (!kPair && LOAD == kDma) {
 #pragma unroll
         for (int i = 0; i < D::kOffsets; ++i) {
-            ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(T) + D::piece(tid, i) * 16);
-            vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(T) + D::piece(tid, i) * 16);
+            ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(E) + D::piece(tid, i) * 16);
+            vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(E) + D::piece(tid, i) * 16);
         }
         if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KT, t1 - t0);
     }
     auto fetch = [&](int tile, int buf) {
-        if constexpr (LOAD == kDma) {
+        if constexpr (kPair) {
+            const int64_t at = (bh * pair_rows(c.m) + (int64_t)tile * KT) * TL::kRow;
+            const unsigned to = lds_address(base) + 2 * buf * kTile;
+            DmaImage<DP, KT, NT>::load(c.pair.img[kPairK] + at, to, tid);
+            DmaImage<DP, KT, NT>::load(c.pair.img[kPairV] + at, to + kTile, tid);
+        } else if constexpr (LOAD == kDma) {
             const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(T), to, tid, c.d, k_len - tile * KT);
-            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(T), to + kTile, tid, c.d, k_len - tile * KT);
+            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(E), to, tid, c.d, k_len - tile * KT);
+            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(E), to + kTile, tid, c.d, k_len - tile * KT);
         } else {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
                 const int p = tid + i * NT, pc = p % TL::kPieces, key = tile * KT + p / TL::kPieces, at = min(key, k_len - 1);
-                kr[i] = load_piece<T, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
-                vr[i] = load_piece<T, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
+                kr[i] = load_piece<E, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
+                vr[i] = load_piece<E, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
                 if (BIAS && bp[at] == -INFINITY) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
             }
-            if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
         }
+        if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
     };
     auto put = [&](int buf) {
-        if constexpr (LOAD != kDma) {
+        if constexpr (!kDirect) {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
                 const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
                 *(uint4 *)(lds + (2 * buf) * kTile + at) = kr[i];
                 *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
             }
-            if (BIAS && tid < KT) lbias[buf][tid] = br;
         }
+        if (BIAS && tid < KT) lbias[buf][tid] = br;
     };
 
     if (t0 < t1) fetch(t0, 0);
     Frag q[NS], g[NS];
     const int head = hk * c.group + pk.g;
-    const int64_t bh = (int64_t)b * c.kv_heads + hk;
     float delta = 0.0f;
     {
-        const T *rq = (const T *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + head * c.sq.head;
-        const T *rg = (const T *)c.d_o + b * c.s_do.batch + (int64_t)pk.q * c.s_do.row + head * c.s_do.head;
-        const T *ro = (const T *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + head * c.so.head;
+        using P = std::conditional_t<kPair, Mma<float>, M>;   // (how the tensors themselves are read)
+        const E *rq = (const E *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + head * c.sq.head;
+        const E *rg = (const E *)c.d_o + b * c.s_do.batch + (int64_t)pk.q * c.s_do.row + head * c.s_do.head;
+        const E *ro = (const E *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + head * c.so.head;
+        const uint4 z = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < NS; ++t) {
-            const uint4 z = make_uint4(0, 0, 0, 0);
-            q[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rq, 2 * t + half, c.d) : z);
-            g[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rg, 2 * t + half, c.d) : z);
-            const Frag o = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(ro, 2 * t + half, c.d) : z);
+        for (int t = 0; t < DP / P::kStep; ++t) {
+            const auto gt = __builtin_bit_cast(typename P::Frag, live ? load_piece<E, ALN>(rg, 2 * t + half, c.d) : z);
+            const auto ot = __builtin_bit_cast(typename P::Frag, live ? load_piece<E, ALN>(ro, 2 * t + half, c.d) : z);
 #pragma unroll
-            for (int j = 0; j < M::kPiece; ++j) delta = fmaf((float)g[t][j], (float)o[j], delta);
+            for (int j = 0; j < P::kPiece; ++j) delta = fmaf((float)gt[j], (float)ot[j], delta);
+            if constexpr (!kPair) {
+                q[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(rq, 2 * t + half, c.d) : z);
+                g[t] = gt;
+            }
+        }
+        if constexpr (kPair) {
+            const int64_t at = bh * pair_rows(rows) * TL::kRow;
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                q[t] = TL::from_image(c.pair.img[kPairQ] + at, r, t, half);
+                g[t] = TL::from_image(c.pair.img[kPairDo] + at, r, t, half);
+            }
         }
     }
     delta = across_halves_sum(delta);
+    if (kPair) delta *= ps.ds;
     RowStat st = {0.0f, INFINITY};
     if (live) {
         const float2 v = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
@@ -138,11 +163,11 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
     if (split == 0 && half == 0) {   // for the other pass, whole blocks of rows
         const int64_t pad = (int64_t)blocks * 32 * WAVES;
         float *out = c.row_stat + 3 * bh * pad + r;
-        out[0] = st.off;
-        out[pad] = delta;
+        out[0] = kPair ? st.off - 15.0f : st.off;   // (probabilities times kPairN = 2^15)
+        out[pad] = kPair ? delta / kPairN : delta;
         if (kDiff) out[2 * pad] = st.m;
     }
-    const float unit = kDiff ? kLog2eF : c.scale * kLog2eF;
+    const float unit = kDiff ? kLog2eF : scale * kLog2eF;
     const typename TL::Lanes ln = TL::lanes(lane);
 
     f32x16 dq[ND];
@@ -170,7 +195,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
                 for (int u = 0; u < 4; ++u) {
                     const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * u + 4 * half];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], c.scale, add[j]);
+                    for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], scale, add[j]);
                 }
             }
             if (masked) {
@@ -181,9 +206,9 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 // (without bias m is taken off in the same fma that scales)
-                const float d = BIAS ? s[i] - st.m : kDiff ? fmaf(s[i], c.scale, -st.m) : s[i];
+                const float d = BIAS ? s[i] - st.m : kDiff ? fmaf(s[i], scale, -st.m) : s[i];
                 const float p = __builtin_amdgcn_exp2f(fmaf(d, unit, -st.off));
-                s[i] = p * (dp[i] - delta);
+                s[i] = p * (kPair ? fmaf(dp[i], ps.dov, -delta) : dp[i] - delta);
             }
 #pragma unroll
             for (int t = 0; t < NF; ++t) {
@@ -192,11 +217,15 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
                 for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, ln, nb * 32, t, i, lane), ds, dq[i]);
             }
         }
-        if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
-        if (LOAD == kDma) dma_wait();
+        if ((!kDirect || BIAS) && tile + 1 < t1) put(buf ^ 1);
+        if (kDirect) dma_wait();
         __syncthreads();
     }
     if (r >= rows) return;
+    if constexpr (kPair) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) dq[i] *= ps.dq;
+    }
     if (c.splits > 1) {
         float *po = c.part + ((int64_t)split * c.batch * c.kv_heads * rows + bh * rows + r) * DP + 4 * half;
 #pragma unroll
@@ -206,22 +235,23 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves(sizeof(T), DP)) void k_attn_dq
                 *(f32x4 *)(po + 32 * i + 8 * u) = f32x4{dq[i][4 * u], dq[i][4 * u + 1], dq[i][4 * u + 2], dq[i][4 * u + 3]};
         return;
     }
-    T *out = (T *)c.dq + b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + head * c.sdq.head;
+    E *out = (E *)c.dq + b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + head * c.sdq.head;
 #pragma unroll
-    for (int i = 0; i < ND; ++i) store_column<T, ALN>(out, dq[i], c.scale, 32 * i + 4 * half, c.d);
+    for (int i = 0; i < ND; ++i) store_column<E, ALN>(out, dq[i], c.scale, 32 * i + 4 * half, c.d);
 }
 
 template <typename T, int DP, int RT, int WAVES, bool BIAS, Load LOAD>
-__global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_dkv(const AttnCall c)
+__global__ __launch_bounds__(64 * WAVES, dkv_waves<T>(DP)) void k_attn_dkv(const AttnCall c)
 {
     using M = Mma<T>;
+    using E = typename M::Elem;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
     using D = Dma<T, DP, RT, 64 * WAVES>;
-    constexpr bool ALN = LOAD != kAny;
+    constexpr bool ALN = LOAD != kAny, kPair = std::is_same<T, Pair>::value, kDirect = kPair || LOAD == kDma;
     constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = RT / 32, NF = 32 / M::kStep, ND = DP / 32;
     constexpr int kTile = D::kTile, NPC = D::kCount;
-    constexpr bool kDiff = BIAS || sizeof(T) == 4;
+    constexpr bool kDiff = BIAS || sizeof(E) == 4;
     constexpr int kStats = kDiff ? 3 : 2;
     static_assert(RT * TL::kPieces % NT == 0 && RT <= 64, "");
     __shared__ __align__(16) char lds[4 * kTile];
@@ -246,20 +276,23 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
     // the first packed row that sees this lane's key
     const int sees = c.causal ? max(0, key - k_len + q_len) * c.group : 0;
 
-    const T *qp = (const T *)c.q + b * c.sq.batch + (int64_t)hk * c.group * c.sq.head;
-    const T *gp = (const T *)c.d_o + b * c.s_do.batch + (int64_t)hk * c.group * c.s_do.head;
+    const E *qp = (const E *)c.q + b * c.sq.batch + (int64_t)hk * c.group * c.sq.head;
+    const E *gp = (const E *)c.d_o + b * c.s_do.batch + (int64_t)hk * c.group * c.s_do.head;
+    PairScale ps;
+    if constexpr (kPair) ps = pair_scale(c, bh);
+    const float scale = kPair ? ps.score : c.scale, dov = kPair ? ps.dov / kPairN : 1.0f;
     const int64_t pad = round_up_rows(rows);
     const float *sp = c.row_stat + 3 * bh * pad;
     const LdsPtr base = (LdsPtr)lds;
 
     unsigned qo[D::kOffsets], go[D::kOffsets];
-    uint4 qr[LOAD == kDma ? 1 : NPC], gr[LOAD == kDma ? 1 : NPC];
+    uint4 qr[kDirect ? 1 : NPC], gr[kDirect ? 1 : NPC];
     float sr[kStats];
     auto offset = [&](int row, const HeadsAt &at, int piece) {   // of a row within its tile, which begins with a whole query
         const Packed pk = unpack(row, c.group);
-        return (unsigned)((pk.q * (int)at.row + pk.g * (int)at.head) * (int)sizeof(T) + piece * 16);
+        return (unsigned)((pk.q * (int)at.row + pk.g * (int)at.head) * (int)sizeof(E) + piece * 16);
     };
-    if constexpr (LOAD == kDma) {
+    if constexpr (!kPair && LOAD == kDma) {
 #pragma unroll
         for (int i = 0; i < D::kOffsets; ++i) {
             qo[i] = offset(D::row(tid, i), c.sq, D::piece(tid, i));
@@ -268,33 +301,40 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
         if (t0 < t1) D::clear(lds, tid, c.d, q_len * c.group - (t1 - 1) * RT, t1 - t0);
     }
     auto fetch = [&](int tile, int buf) {
-        if constexpr (LOAD == kDma) {
+        if constexpr (kPair) {
+            const int64_t at = (bh * pair_rows(rows) + (int64_t)tile * RT) * TL::kRow;
+            const unsigned to = lds_address(base) + 2 * buf * kTile;
+            DmaImage<DP, RT, NT>::load(c.pair.img[kPairQ] + at, to, tid);
+            DmaImage<DP, RT, NT>::load(c.pair.img[kPairDo] + at, to + kTile, tid);
+        } else if constexpr (LOAD == kDma) {
             const int64_t q0 = tile * RT / c.group;
             const char *qb = (const char *)(qp + q0 * c.sq.row), *gb = (const char *)(gp + q0 * c.s_do.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
             const int queries = D::kRound / c.group, left = q_len * c.group - tile * RT;   // (a round is whole queries: see launch_attn_grad)
-            D::load(qb, qo, queries * c.sq.row * (int)sizeof(T), to, tid, c.d, left);
-            D::load(gb, go, queries * c.s_do.row * (int)sizeof(T), to + kTile, tid, c.d, left);
-            if (__builtin_amdgcn_readfirstlane(wave) == 0 && lane < RT) {
-                const unsigned at = __builtin_amdgcn_readfirstlane(lds_address((LdsPtr)(const char *)&lstat[buf][0][0]));
-#pragma unroll
-                for (int k = 0; k < kStats; ++k) dma4s(sp + k * pad + (int64_t)tile * RT, 4 * lane, at + k * RT * 4);
-            }
+            D::load(qb, qo, queries * c.sq.row * (int)sizeof(E), to, tid, c.d, left);
+            D::load(gb, go, queries * c.s_do.row * (int)sizeof(E), to + kTile, tid, c.d, left);
         } else {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
                 const int p = tid + i * NT, pc = p % TL::kPieces;
                 const Packed pk = unpack(min(tile * RT + p / TL::kPieces, q_len * c.group - 1), c.group);
-                qr[i] = load_piece<T, ALN>(qp + (int64_t)pk.q * c.sq.row + pk.g * c.sq.head, pc, c.d);
-                gr[i] = load_piece<T, ALN>(gp + (int64_t)pk.q * c.s_do.row + pk.g * c.s_do.head, pc, c.d);
+                qr[i] = load_piece<E, ALN>(qp + (int64_t)pk.q * c.sq.row + pk.g * c.sq.head, pc, c.d);
+                gr[i] = load_piece<E, ALN>(gp + (int64_t)pk.q * c.s_do.row + pk.g * c.s_do.head, pc, c.d);
             }
             if (tid < RT)
 #pragma unroll
                 for (int k = 0; k < kStats; ++k) sr[k] = sp[k * pad + tile * RT + tid];
         }
+        if constexpr (kDirect) {
+            if (__builtin_amdgcn_readfirstlane(wave) == 0 && lane < RT) {
+                const unsigned at = __builtin_amdgcn_readfirstlane(lds_address((LdsPtr)(const char *)&lstat[buf][0][0]));
+#pragma unroll
+                for (int k = 0; k < kStats; ++k) dma4s(sp + k * pad + (int64_t)tile * RT, 4 * lane, at + k * RT * 4);
+            }
+        }
     };
     auto put = [&](int buf) {
-        if constexpr (LOAD != kDma) {
+        if constexpr (!kDirect) {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
                 const int p = tid + i * NT, at = TL::at(p / TL::kPieces, p % TL::kPieces);
@@ -309,17 +349,24 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
 
     if (t0 < t1) fetch(t0, 0);
     Frag k[NS], v[NS];
-    {
-        const T *rk = (const T *)c.k + b * c.sk.batch + (int64_t)key * c.sk.row + hk * c.sk.head;
-        const T *rv = (const T *)c.v + b * c.sv.batch + (int64_t)key * c.sv.row + hk * c.sv.head;
+    if constexpr (kPair) {
+        const int64_t at = bh * pair_rows(c.m) * TL::kRow;
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            k[t] = TL::from_image(c.pair.img[kPairK] + at, key, t, half);
+            v[t] = TL::from_image(c.pair.img[kPairV] + at, key, t, half);
+        }
+    } else {
+        const E *rk = (const E *)c.k + b * c.sk.batch + (int64_t)key * c.sk.row + hk * c.sk.head;
+        const E *rv = (const E *)c.v + b * c.sv.batch + (int64_t)key * c.sv.row + hk * c.sv.head;
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
             const uint4 z = make_uint4(0, 0, 0, 0);
-            k[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rk, 2 * t + half, c.d) : z);
-            v[t] = __builtin_bit_cast(Frag, live ? load_piece<T, ALN>(rv, 2 * t + half, c.d) : z);
+            k[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(rk, 2 * t + half, c.d) : z);
+            v[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(rv, 2 * t + half, c.d) : z);
         }
     }
-    const float unit = kDiff ? kLog2eF : c.scale * kLog2eF;
+    const float unit = kDiff ? kLog2eF : scale * kLog2eF;
     const typename TL::Lanes ln = TL::lanes(lane);
 
     f32x16 dk[ND], dv[ND];
@@ -344,7 +391,7 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
             for (int t = 0; t < NS; ++t) s = M::mma(TL::rows(lq, ln, nb * 32, t), k[t], s);
             if constexpr (BIAS) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], c.scale, bias);
+                for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale, bias);
             }
             if (masked) {
                 const int base = tile * RT + nb * 32 + 4 * half;
@@ -360,7 +407,7 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * u + j;
-                    const float d = BIAS ? s[i] - m[j] : kDiff ? fmaf(s[i], c.scale, -m[j]) : s[i];
+                    const float d = BIAS ? s[i] - m[j] : kDiff ? fmaf(s[i], scale, -m[j]) : s[i];
                     s[i] = __builtin_amdgcn_exp2f(fmaf(d, unit, -off[j]));
                 }
             }
@@ -380,7 +427,7 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * u + j;
-                    s[i] *= dp[i] - dl[j];
+                    s[i] *= kPair ? fmaf(dp[i], dov, -dl[j]) : dp[i] - dl[j];
                     if (BIAS) db += s[i];
                 }
             }
@@ -393,8 +440,8 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (LOAD != kDma && tile + 1 < t1) put(buf ^ 1);
-        if (LOAD == kDma) dma_wait();
+        if (!kDirect && tile + 1 < t1) put(buf ^ 1);
+        if (kDirect) dma_wait();
         __syncthreads();
     }
     if (BIAS) db = across_halves_sum(db);
@@ -403,6 +450,14 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
 #pragma unroll
         for (int i = 0; i < ND; ++i) dk[i] = dv[i] = (f32x16)(0.0f);
         db = 0.0f;
+    }
+    if constexpr (kPair) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            dk[i] *= ps.dk;
+            dv[i] *= ps.dv;
+        }
+        db /= ps.ds;
     }
     const int64_t slot = ((int64_t)split * c.batch * c.kv_heads + bh) * c.m + key;
     if (BIAS && c.dbias && half == 0) c.dbias_part[slot] = db;
@@ -417,12 +472,12 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves(sizeof(T), DP)) void k_attn_d
             }
         return;
     }
-    T *ok = (T *)c.dk + b * c.sdk.batch + (int64_t)key * c.sdk.row + hk * c.sdk.head;
-    T *ov = (T *)c.dv + b * c.sdv.batch + (int64_t)key * c.sdv.row + hk * c.sdv.head;
+    E *ok = (E *)c.dk + b * c.sdk.batch + (int64_t)key * c.sdk.row + hk * c.sdk.head;
+    E *ov = (E *)c.dv + b * c.sdv.batch + (int64_t)key * c.sdv.row + hk * c.sdv.head;
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-        store_column<T, ALN>(ok, dk[i], c.scale, 32 * i + 4 * half, c.d);
-        store_column<T, ALN>(ov, dv[i], 1.0f, 32 * i + 4 * half, c.d);
+        store_column<E, ALN>(ok, dk[i], c.scale, 32 * i + 4 * half, c.d);
+        store_column<E, ALN>(ov, dv[i], 1.0f, 32 * i + 4 * half, c.d);
     }
 }
 
@@ -497,7 +552,9 @@ template <typename T> __global__ __launch_bounds__(256) void k_attn_dbias(const 
 template <typename T, int DP>
 fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Load rows_load)
 {
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, RT = row_tile(sizeof(T));
+    using E = typename Mma<T>::Elem;
+    constexpr bool kPair = std::is_same<T, Pair>::value;
+    constexpr int RT = row_tile<T>(DP), KT = RT;
     Arena A;
     a.row_stat = (float *)(ws + A.take(p.stat_bytes));
     float *dq_part = (float *)(ws + A.take(p.dq_bytes)), *dkv_part = (float *)(ws + A.take(p.dkv_bytes));
@@ -510,27 +567,36 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
             if (keys != kAny) k_attn_dq<T, DP, KT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dq<T, DP, KT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
         } else {
-            if (keys == kDma) k_attn_dq<T, DP, KT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
-            else if (keys == kVec) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if constexpr (!kPair) {
+                if (keys == kDma) k_attn_dq<T, DP, KT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
+            }
+            if (keys == kDma && !kPair) {
+            } else if (keys != kAny) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dq<T, DP, KT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
-        if (a.splits > 1) join<T, DP, false>(c, a);
+        if (a.splits > 1) join<E, DP, false>(c, a);
     }
     a.splits = p.k_splits;
     a.part = dkv_part;
     if (p.k_grid) {
         const unsigned grid = (unsigned)p.k_grid;
         if (a.bias) {
-            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, true, kDma><<<grid, 256, 0, c->stream>>>(a);
-            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if constexpr (!kPair) {
+                if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, true, kDma><<<grid, 256, 0, c->stream>>>(a);
+            }
+            if (rows_load == kDma && !kPair) {
+            } else if (rows_load != kAny) k_attn_dkv<T, DP, RT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dkv<T, DP, RT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
         } else {
-            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
-            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if constexpr (!kPair) {
+                if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
+            }
+            if (rows_load == kDma && !kPair) {
+            } else if (rows_load != kAny) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dkv<T, DP, RT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
-        if (a.splits > 1) join<T, DP, true>(c, a);
-        if (a.dbias) k_attn_dbias<T><<<(unsigned)ceil_div((int64_t)a.batch * a.m, 256), 256, 0, c->stream>>>(a);
+        if (a.splits > 1) join<E, DP, true>(c, a);
+        if (a.dbias) k_attn_dbias<E><<<(unsigned)ceil_div((int64_t)a.batch * a.m, 256), 256, 0, c->stream>>>(a);
     }
     FS_HIP(c, hipGetLastError());
     return FS_OK;
@@ -554,7 +620,9 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
     const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads, dp = round_up(a.d, 32);
     const int64_t want = 2 * (int64_t)c->num_cu;
     const int64_t qb = ceil_div(rows, 128) * heads, kb = ceil_div(a.m, 128) * heads;
-    const int64_t kt = ceil_div(a.m, f32 ? 32 : 64), rt = ceil_div(rows, row_tile(f32 ? 4 : 2));
+    p.pairs = f32 && pair_worth(c, a, true);
+    const int tile = !f32 || (p.pairs && dp <= 64) ? 64 : 32;
+    const int64_t kt = ceil_div(a.m, tile), rt = ceil_div(rows, tile);
     p.q_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(qb, 1), kt / 4));
     // (under a causal line blocks are of unequal length: twice as many, so that short ones fill up behind long ones)
     p.k_splits = (int)std::max<int64_t>(1, std::min((a.causal ? 2 : 1) * want / std::max<int64_t>(kb, 1), rt / 4));
@@ -563,6 +631,7 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
     p.stat_bytes = (size_t)(heads * round_up(rows, kRowBlock)) * 12;
     p.dq_bytes = p.q_splits > 1 ? (size_t)(heads * rows * dp * p.q_splits) * 4 : 0;
     p.dkv_bytes = p.k_splits > 1 ? (size_t)(heads * a.m * dp * 2 * p.k_splits) * 4 : 0;
+    p.pair_bytes = p.pairs ? pair_bytes(a, true) : 0;
     p.dbias_bytes = a.dbias ? (size_t)(heads * a.m * p.k_splits) * 4 : 0;
     return p;
 }
@@ -573,9 +642,13 @@ fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, 
     const int64_t kmost = std::max(a.sk.row, a.sv.row) * es * 64;
     const Load keys = !aligned ? kAny : kmost < (int64_t(1) << 31) ? kDma : kVec;
     // tiles of rows, and the rounds that load them, begin with a whole query
-    const int rt = row_tile(es), dp = (int)round_up(a.d, 32), round = dp == 96 ? rt : std::min(rt, 256 * 16 / dp / es);
+    const int rt = f32 ? 32 : 64, dp = (int)round_up(a.d, 32), round = dp == 96 ? rt : std::min(rt, 256 * 16 / dp / es);
     const int64_t rmost = (std::max(a.sq.row, a.s_do.row) * rt / a.group + std::max(a.sq.head, a.s_do.head) * a.group) * es;
     const Load rows = !aligned ? kAny : rt % a.group == 0 && round % a.group == 0 && rmost < (int64_t(1) << 31) ? kDma : kVec;
+    if (p.pairs) {
+        const fs_status st = launch_pairs(c, a, true);
+        return st ? st : by_width<Pair>(c, a, p, ws, aligned ? kVec : kAny, aligned ? kVec : kAny);
+    }
     return f32 ? by_width<float>(c, a, p, ws, keys, rows) : by_width<__bf16>(c, a, p, ws, keys, rows);
 }
 

@@ -1,0 +1,189 @@
+// Floats as pairs of fp16 for attention in full precision (see Pair in fs_attn.h): two passes over q, k, v and do, one for the largest
+// magnitude (and row norm) of every head, one that writes the pieces as the attention kernels' LDS tiles.  Any strides, lengths and
+// removed keys end here: what is not admitted becomes zero.
+#include <algorithm>
+
+#include "fs_attn.h"
+
+namespace fs {
+namespace {
+
+// rows of a workgroup of the first pass: 128, or so many that there are at most 512 workgroups
+__host__ __device__ inline int chunk_rows(int64_t rows) { return rows <= 512 * 128 ? 128 : (int)((rows + 511) / 512); }
+__host__ __device__ inline int chunks(int64_t rows) { return (int)((rows + chunk_rows(rows) - 1) / chunk_rows(rows)); }
+
+struct Rows {
+    const float *p;      // row 0 of this (set, kv head), nullptr: not admitted
+    HeadsAt at;
+    bool keys;
+    int count;           // packed rows, or keys
+};
+__device__ inline Rows rows_of(const AttnCall &c, int tensor, int bh)
+{
+    const int b = bh / c.kv_heads, hk = bh - b * c.kv_heads;
+    const HeadsAt at = tensor == kPairQ ? c.sq : tensor == kPairK ? c.sk : tensor == kPairV ? c.sv : c.s_do;
+    const void *p = tensor == kPairQ ? c.q : tensor == kPairK ? c.k : tensor == kPairV ? c.v : c.d_o;
+    const bool keys = tensor == kPairK || tensor == kPairV;
+    return {(const float *)p + b * at.batch + (int64_t)(keys ? hk : hk * c.group) * at.head, at, keys, keys ? c.m : c.n * c.group};
+}
+__device__ inline const float *row_at(const AttnCall &c, const Rows &t, int b, int r)
+{
+    if (t.keys) {
+        const int len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
+        if (r >= len || (c.bias && c.bias[b * c.bias_ld + r] == -INFINITY)) return nullptr;
+        return t.p + (int64_t)r * t.at.row;
+    }
+    const Packed pk = unpack(r, c.group);
+    const int len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
+    return pk.q < len ? t.p + (int64_t)pk.q * t.at.row + pk.g * t.at.head : nullptr;
+}
+
+// sixteen lanes take a row
+__global__ __launch_bounds__(256) void k_pair_max(const AttnCall c)
+{
+    __shared__ float2 lds[4];
+    const int bh = blockIdx.y, tensor = blockIdx.z, heads = c.batch * c.kv_heads;
+    const Rows t = rows_of(c, tensor, bh);
+    const int per = chunk_rows(t.count), r0 = blockIdx.x * per, r1 = min(t.count, r0 + per), x = threadIdx.x & 15;
+    if (r0 >= t.count) return;
+    float top = 0.0f, norm = 0.0f;
+    for (int r = r0 + threadIdx.x / 16; r < r1; r += 16) {
+        const float *row = row_at(c, t, bh / c.kv_heads, r);
+        double s = 0.0;   // (squares leave a float's range before the values do)
+        if (row)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = x + 16 * j < c.d ? fabsf(row[x + 16 * j]) : 0.0f;
+                if (v < INFINITY) {   // (what is not finite spreads by itself)
+                    top = fmaxf(top, v);
+                    s = fma((double)v, (double)v, s);
+                }
+            }
+#pragma unroll
+        for (int m = 1; m < 16; m *= 2) s += __shfl_xor(s, m);
+        norm = fmaxf(norm, (float)sqrt(s));
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        top = fmaxf(top, __shfl_xor(top, m));
+        norm = fmaxf(norm, __shfl_xor(norm, m));
+    }
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(top, norm);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 4; ++i) lds[0] = make_float2(fmaxf(lds[0].x, lds[i].x), fmaxf(lds[0].y, lds[i].y));
+        ((float2 *)c.pair.part)[((int64_t)tensor * heads + bh) * 512 + blockIdx.x] = lds[0];
+    }
+}
+
+// the power of two that puts `top` into [2^14, 2^15)
+__device__ inline float scale_of(float top)
+{
+    if (top == 0.0f) return 1.0f;
+    int e = 127 + 14 - ((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127);
+    e = e < 1 ? 1 : e > 240 ? 240 : e;
+    return __builtin_bit_cast(float, (uint32_t)e << 23);
+}
+
+// a workgroup writes 32 rows
+template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const AttnCall c)
+{
+    using TL = Tile<Pair, DP>;
+    __shared__ float2 lds[4];
+    const int bh = blockIdx.y, tensor = blockIdx.z, heads = c.batch * c.kv_heads;
+    const Rows t = rows_of(c, tensor, bh);
+    const int64_t pad = pair_rows(t.count);
+    if ((int64_t)blockIdx.x * 32 >= pad) return;
+    float top = 0.0f, norm = 0.0f;
+    for (int i = threadIdx.x; i < chunks(t.count); i += 256) {
+        const float2 v = ((const float2 *)c.pair.part)[((int64_t)tensor * heads + bh) * 512 + i];
+        top = fmaxf(top, v.x);
+        norm = fmaxf(norm, v.y);
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        top = fmaxf(top, __shfl_xor(top, m));
+        norm = fmaxf(norm, __shfl_xor(norm, m));
+    }
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(top, norm);
+    __syncthreads();
+    top = fmaxf(fmaxf(lds[0].x, lds[1].x), fmaxf(lds[2].x, lds[3].x));
+    norm = fmaxf(fmaxf(lds[0].y, lds[1].y), fmaxf(lds[2].y, lds[3].y));
+    const float scale = scale_of(top);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        c.pair.scale[8 * bh + tensor] = scale;
+        if (tensor >= kPairV) c.pair.scale[8 * bh + 4 + tensor - kPairV] = norm;
+    }
+    char *img = c.pair.img[tensor] + ((int64_t)bh * pad + (int64_t)blockIdx.x * 32) * TL::kRow;
+    for (int p = threadIdx.x; p < 32 * DP / 8; p += 256) {
+        const int r = p / (DP / 8), piece = p % (DP / 8), row_id = blockIdx.x * 32 + r;
+        const float *row = row_id < t.count ? row_at(c, t, bh / c.kv_heads, row_id) : nullptr;
+        f16x8 h, l;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            _Float16 a = (_Float16)0.0f, b = (_Float16)0.0f;
+            if (row && piece * 8 + j < c.d) Mma<Pair>::split(row[piece * 8 + j] * scale, a, b);
+            h[j] = a;
+            l[j] = b;
+        }
+        const int at = TL::B::at(r, piece);
+        *(f16x8 *)(img + at) = h;
+        *(f16x8 *)(img + TL::kLower + at) = l;
+    }
+}
+
+int64_t image_bytes(const AttnCall &a, int tensor)
+{
+    const bool keys = tensor == kPairK || tensor == kPairV;
+    return (int64_t)a.batch * a.kv_heads * pair_rows(keys ? a.m : (int64_t)a.n * a.group) * round_up(a.d, 32) * 4;
+}
+
+}  // namespace
+
+// The two passes and the pieces' way through memory take some 12 us; the products on the fp32 matrix cores run at 90 to 100 TFLOP/s, those
+// of pairs at several times that.  A few rows, bound by memory, gain nothing.
+bool pair_worth(const Ctx *c, const AttnCall &a, bool grad)
+{
+    const int64_t rows = (int64_t)a.n * a.group;
+    if (rows == 0 || a.m == 0 || (int64_t)a.batch * a.kv_heads > 65535) return false;
+    if (c->dbg_attn_pairs) return c->dbg_attn_pairs == 1;
+    return rows > 32 && (grad ? 2.5 : 1.0) * 4.0 * (double)a.batch * a.kv_heads * rows * a.m * a.d * (a.causal ? 0.5 : 1.0) >= 1.5e9;
+}
+
+size_t pair_bytes(const AttnCall &a, bool grad)
+{
+    AttnCall t = a;
+    pair_layout(&t, nullptr, grad);
+    return (size_t)((char *)t.pair.part - (char *)nullptr) + (size_t)kPairTensors * a.batch * a.kv_heads * 512 * 8;
+}
+
+void pair_layout(AttnCall *a, char *ws, bool grad)
+{
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char *p = (char *)((uintptr_t)ws + at);
+        at += (bytes + 255) & ~size_t(255);
+        return p;
+    };
+    for (int t = 0; t < kPairTensors; ++t) a->pair.img[t] = t < kPairDo || grad ? take((size_t)image_bytes(*a, t)) : nullptr;
+    a->pair.scale = (float *)take((size_t)a->batch * a->kv_heads * 32);
+    a->pair.part = (float *)take(0);
+}
+
+fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad)
+{
+    const int64_t most = std::max<int64_t>(a.m, (int64_t)a.n * a.group);
+    const unsigned heads = (unsigned)(a.batch * a.kv_heads), tensors = grad ? 4 : 3;
+    k_pair_max<<<dim3((unsigned)std::max(chunks(a.m), chunks((int64_t)a.n * a.group)), heads, tensors), 256, 0, c->stream>>>(a);
+    const dim3 grid((unsigned)(pair_rows(most) / 32), heads, tensors);
+    switch ((a.d + 31) / 32) {
+    case 1: k_pair_split<32><<<grid, 256, 0, c->stream>>>(a); break;
+    case 2: k_pair_split<64><<<grid, 256, 0, c->stream>>>(a); break;
+    case 3: k_pair_split<96><<<grid, 256, 0, c->stream>>>(a); break;
+    default: k_pair_split<128><<<grid, 256, 0, c->stream>>>(a); break;
+    }
+    FS_HIP(c, hipGetLastError());
+    return FS_OK;
+}
+
+}  // namespace fs

@@ -250,6 +250,7 @@ struct Ctx {
     int dbg_fx_splits = 0;           // forced split count of the streamed side of a fixed-point pass
     int dbg_fx_long = 0;             // 1: fixed-point half-steps of any length as long ones (MODE 3 or 4), 2: none
     unsigned long long *fx_count = nullptr;   // device: tiles that long half-steps have left at their leading products, and all of theirs
+    int dbg_attn_pairs = 0;          // float32 attention through pairs of fp16: 1: always, 2: never
     int dbg_moment_kind = 0;         // 1 + the expansion that passes through cell moments take
     int moment_kind = 0;             // 1 + the one that the last such pass took
     // profiling of the streaming LSE launches
