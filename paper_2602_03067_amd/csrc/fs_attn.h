@@ -22,6 +22,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 template <typename T> struct Mma;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // Floats as the sum of two fp16, under a power of two for all of a head's rows that puts the largest into [2^14, 2^15): 22 bits of
 // every element down to 2^-17 of the largest, and never less than 2^-40 of it.  A product takes three products of the pieces
@@ -41,23 +42,26 @@ template <> struct Mma<Pair> {
         c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.h, b.l, c, 0, 0, 0);
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.h, b.h, c, 0, 0, 0);
     }
-    static __device__ inline void split(float v, _Float16 &h, _Float16 &l)
+    // two elements: their upper pieces, and what is left of each
+    static __device__ inline void split(float a, float b, f16x2 &h, f16x2 &l)
     {
-        // v as a float first: where a product is converted, one instruction may round it to fp16 at once, which near a tie is not the
+        // as floats first: where a product is converted, one instruction may round it to fp16 at once, which near a tie is not the
         // upper piece that the lower one was taken off
-        asm volatile("" : "+v"(v));
-        h = (_Float16)v;
-        l = (_Float16)(v - (float)h);
+        asm volatile("" : "+v"(a), "+v"(b));
+        h = f16x2{(_Float16)a, (_Float16)b};
+        l = f16x2{(_Float16)fmaf((float)h[0], -1.0f, a), (_Float16)fmaf((float)h[1], -1.0f, b)};
     }
     static __device__ inline Frag pack(const f32x16 &v, int t)
     {
         Frag f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            _Float16 h, l;
-            split(v[8 * t + j], h, l);
-            f.h[j] = h;
-            f.l[j] = l;
+        for (int j = 0; j < 8; j += 2) {
+            f16x2 h, l;
+            split(v[8 * t + j], v[8 * t + j + 1], h, l);
+            f.h[j] = h[0];
+            f.h[j + 1] = h[1];
+            f.l[j] = l[0];
+            f.l[j + 1] = l[1];
         }
         return f;
     }
@@ -368,7 +372,7 @@ __device__ inline Work work_of(int id, int total, int splits, int blocks, int kv
 bool pair_worth(const Ctx *c, const AttnCall &a, bool grad);
 size_t pair_bytes(const AttnCall &a, bool grad);
 void pair_layout(AttnCall *a, char *ws, bool grad);
-fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad);
+fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad, bool aligned);
 
 // how a forward pass is launched
 struct AttnPlan {

@@ -125,9 +125,10 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
     for (int i = 0; i < ND; ++i) o[i] = (f32x16)(0.0f);
     // units of the running values: without bias the products <q, k>, with it the scores
     const float unit = BIAS ? kLog2eF : scale * kLog2eF;
-    // exp2((s - ref) unit), the difference first: a bias of the type's lowest value times log2 e would leave the type, and full
-    // precision is not to lose an ulp of the larger of the two.  In bf16 without bias one fma does.
-    constexpr bool kDiff = BIAS || sizeof(E) == 4;
+    // exp2((s - ref) unit), the difference first: a bias of the type's lowest value times log2 e would leave the type.  Without bias one
+    // fma does, whose reference is rounded once for the whole row (the fp32 matrix cores, which wait for nobody, keep the difference:
+    // a row of one key then is that key's value to the last bit).
+    constexpr bool kDiff = BIAS || std::is_same<T, float>::value;
     float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
     const typename TL::Lanes ln = TL::lanes(lane);
 
@@ -173,14 +174,13 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
     // their exponentials into the sum and, times the values, into the accumulators
     auto accumulate = [&](int tile, f32x16 (&s)[NB]) {
         const LdsPtr lv = base + 2 * ((tile - t0) & 1) * kTile + kTile;
-        const float safe = ref == -INFINITY ? 0.0f : ref, off = safe * unit;
+        const float safe = ref == -INFINITY ? 0.0f : ref, off = safe * unit - (kPair ? 4.0f : 0.0f);   // (kPairP = 2^4)
         float part = 0.0f;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float e = kPair ? __builtin_amdgcn_exp2f(fmaf(s[nb][i] - safe, unit, 4.0f))   // kPairP = 2^4
-                              : kDiff ? __builtin_amdgcn_exp2f((s[nb][i] - safe) * unit)
+                const float e = kDiff ? __builtin_amdgcn_exp2f(kPair ? fmaf(s[nb][i] - safe, unit, 4.0f) : (s[nb][i] - safe) * unit)
                                       : __builtin_amdgcn_exp2f(fmaf(s[nb][i], unit, -off));
                 s[nb][i] = e;
                 part += e;
@@ -404,7 +404,7 @@ fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bo
     const int64_t most = std::max(a.sk.row, a.sv.row) * (f32 ? 4 : 2) * 64;
     const Load load = !aligned ? kAny : most < (int64_t(1) << 31) ? kDma : kVec;
     if (p.pairs) {
-        const fs_status st = launch_pairs(c, a, false);
+        const fs_status st = launch_pairs(c, a, false, aligned);
         return st ? st : pairs_by_width(c, a, load, p.grid);
     }
     return f32 ? by_width<float>(c, a, load, p.waves, p.grid) : by_width<__bf16>(c, a, load, p.waves, p.grid);

@@ -646,7 +646,7 @@ fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, 
     const int64_t rmost = (std::max(a.sq.row, a.s_do.row) * rt / a.group + std::max(a.sq.head, a.s_do.head) * a.group) * es;
     const Load rows = !aligned ? kAny : rt % a.group == 0 && round % a.group == 0 && rmost < (int64_t(1) << 31) ? kDma : kVec;
     if (p.pairs) {
-        const fs_status st = launch_pairs(c, a, true);
+        const fs_status st = launch_pairs(c, a, true, aligned);
         return st ? st : by_width<Pair>(c, a, p, ws, aligned ? kVec : kAny, aligned ? kVec : kAny);
     }
     return f32 ? by_width<float>(c, a, p, ws, keys, rows) : by_width<__bf16>(c, a, p, ws, keys, rows);

@@ -8,8 +8,8 @@
 namespace fs {
 namespace {
 
-// rows of a workgroup of the first pass: 128, or so many that there are at most 512 workgroups
-__host__ __device__ inline int chunk_rows(int64_t rows) { return rows <= 512 * 128 ? 128 : (int)((rows + 511) / 512); }
+// rows of a workgroup of the first pass: 32, or so many that a head has at most 512 workgroups
+__host__ __device__ inline int chunk_rows(int64_t rows) { return rows <= 512 * 32 ? 32 : (int)((rows + 511) / 512); }
 __host__ __device__ inline int chunks(int64_t rows) { return (int)((rows + chunk_rows(rows) - 1) / chunk_rows(rows)); }
 
 struct Rows {
@@ -38,29 +38,45 @@ __device__ inline const float *row_at(const AttnCall &c, const Rows &t, int b, i
     return pk.q < len ? t.p + (int64_t)pk.q * t.at.row + pk.g * t.at.head : nullptr;
 }
 
-// sixteen lanes take a row
-__global__ __launch_bounds__(256) void k_pair_max(const AttnCall c)
+// `count` elements of a row from `col` on, zero beyond d (ALN: aligned to 16 bytes, d a multiple of four)
+template <int N> __device__ inline void load_row(const float *row, int col, int d, bool aligned, float (&v)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (row && aligned) {
+            if (col + j < d) u = *(const f32x4 *)(row + col + j);
+        } else if (row) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + j + k < d) u[k] = row[col + j + k];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[j + k] = u[k];
+    }
+}
+
+// eight lanes take a row, each DP / 8 elements of it; a workgroup 32 rows at a time
+template <int DP> __global__ __launch_bounds__(256) void k_pair_max(const AttnCall c, bool aligned)
 {
     __shared__ float2 lds[4];
     const int bh = blockIdx.y, tensor = blockIdx.z, heads = c.batch * c.kv_heads;
     const Rows t = rows_of(c, tensor, bh);
-    const int per = chunk_rows(t.count), r0 = blockIdx.x * per, r1 = min(t.count, r0 + per), x = threadIdx.x & 15;
+    const int per = chunk_rows(t.count), r0 = blockIdx.x * per, r1 = min(t.count, r0 + per), x = threadIdx.x & 7;
     if (r0 >= t.count) return;
     float top = 0.0f, norm = 0.0f;
-    for (int r = r0 + threadIdx.x / 16; r < r1; r += 16) {
-        const float *row = row_at(c, t, bh / c.kv_heads, r);
+    for (int r = r0 + threadIdx.x / 8; r < r1; r += 32) {
+        float v[DP / 8];
+        load_row<DP / 8>(row_at(c, t, bh / c.kv_heads, r), x * (DP / 8), c.d, aligned, v);
         double s = 0.0;   // (squares leave a float's range before the values do)
-        if (row)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float v = x + 16 * j < c.d ? fabsf(row[x + 16 * j]) : 0.0f;
-                if (v < INFINITY) {   // (what is not finite spreads by itself)
-                    top = fmaxf(top, v);
-                    s = fma((double)v, (double)v, s);
-                }
+        for (int j = 0; j < DP / 8; ++j)
+            if (fabsf(v[j]) < INFINITY) {   // (what is not finite spreads by itself)
+                top = fmaxf(top, fabsf(v[j]));
+                s = fma((double)v[j], (double)v[j], s);
             }
 #pragma unroll
-        for (int m = 1; m < 16; m *= 2) s += __shfl_xor(s, m);
+        for (int m = 1; m < 8; m *= 2) s += __shfl_xor(s, m);
         norm = fmaxf(norm, (float)sqrt(s));
     }
 #pragma unroll
@@ -86,7 +102,7 @@ __device__ inline float scale_of(float top)
 }
 
 // a workgroup writes 32 rows
-template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const AttnCall c)
+template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const AttnCall c, bool aligned)
 {
     using TL = Tile<Pair, DP>;
     __shared__ float2 lds[4];
@@ -94,6 +110,13 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const Attn
     const Rows t = rows_of(c, tensor, bh);
     const int64_t pad = pair_rows(t.count);
     if ((int64_t)blockIdx.x * 32 >= pad) return;
+    constexpr int P = 32 * DP / 8, N = (P + 255) / 256;   // pieces of eight elements
+    float v[N][8];   // (on their way while the scale is found)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int p = threadIdx.x + 256 * i, r = blockIdx.x * 32 + p / (DP / 8);
+        load_row<8>(p < P && r < t.count ? row_at(c, t, bh / c.kv_heads, r) : nullptr, p % (DP / 8) * 8, c.d, aligned, v[i]);
+    }
     float top = 0.0f, norm = 0.0f;
     for (int i = threadIdx.x; i < chunks(t.count); i += 256) {
         const float2 v = ((const float2 *)c.pair.part)[((int64_t)tensor * heads + bh) * 512 + i];
@@ -115,18 +138,21 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const Attn
         if (tensor >= kPairV) c.pair.scale[8 * bh + 4 + tensor - kPairV] = norm;
     }
     char *img = c.pair.img[tensor] + ((int64_t)bh * pad + (int64_t)blockIdx.x * 32) * TL::kRow;
-    for (int p = threadIdx.x; p < 32 * DP / 8; p += 256) {
-        const int r = p / (DP / 8), piece = p % (DP / 8), row_id = blockIdx.x * 32 + r;
-        const float *row = row_id < t.count ? row_at(c, t, bh / c.kv_heads, row_id) : nullptr;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int p = threadIdx.x + 256 * i;
+        if (p >= P) break;
         f16x8 h, l;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            _Float16 a = (_Float16)0.0f, b = (_Float16)0.0f;
-            if (row && piece * 8 + j < c.d) Mma<Pair>::split(row[piece * 8 + j] * scale, a, b);
-            h[j] = a;
-            l[j] = b;
+        for (int j = 0; j < 8; j += 2) {
+            f16x2 a, b;
+            Mma<Pair>::split(v[i][j] * scale, v[i][j + 1] * scale, a, b);
+            h[j] = a[0];
+            h[j + 1] = a[1];
+            l[j] = b[0];
+            l[j + 1] = b[1];
         }
-        const int at = TL::B::at(r, piece);
+        const int at = TL::B::at(p / (DP / 8), p % (DP / 8));
         *(f16x8 *)(img + at) = h;
         *(f16x8 *)(img + TL::kLower + at) = l;
     }
@@ -170,17 +196,21 @@ void pair_layout(AttnCall *a, char *ws, bool grad)
     a->pair.part = (float *)take(0);
 }
 
-fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad)
+template <int DP> static void make_pairs(Ctx *c, const AttnCall &a, bool grad, bool aligned)
 {
-    const int64_t most = std::max<int64_t>(a.m, (int64_t)a.n * a.group);
+    const int64_t rows = (int64_t)a.n * a.group;
     const unsigned heads = (unsigned)(a.batch * a.kv_heads), tensors = grad ? 4 : 3;
-    k_pair_max<<<dim3((unsigned)std::max(chunks(a.m), chunks((int64_t)a.n * a.group)), heads, tensors), 256, 0, c->stream>>>(a);
-    const dim3 grid((unsigned)(pair_rows(most) / 32), heads, tensors);
+    k_pair_max<DP><<<dim3((unsigned)std::max(chunks(a.m), chunks(rows)), heads, tensors), 256, 0, c->stream>>>(a, aligned);
+    k_pair_split<DP><<<dim3((unsigned)(pair_rows(std::max<int64_t>(a.m, rows)) / 32), heads, tensors), 256, 0, c->stream>>>(a, aligned);
+}
+
+fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad, bool aligned)
+{
     switch ((a.d + 31) / 32) {
-    case 1: k_pair_split<32><<<grid, 256, 0, c->stream>>>(a); break;
-    case 2: k_pair_split<64><<<grid, 256, 0, c->stream>>>(a); break;
-    case 3: k_pair_split<96><<<grid, 256, 0, c->stream>>>(a); break;
-    default: k_pair_split<128><<<grid, 256, 0, c->stream>>>(a); break;
+    case 1: make_pairs<32>(c, a, grad, aligned); break;
+    case 2: make_pairs<64>(c, a, grad, aligned); break;
+    case 3: make_pairs<96>(c, a, grad, aligned); break;
+    default: make_pairs<128>(c, a, grad, aligned); break;
     }
     FS_HIP(c, hipGetLastError());
     return FS_OK;
