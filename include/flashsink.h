@@ -394,7 +394,7 @@ fs_status fs_points_release(fs_ctx *ctx);
  * kv_heads divides q_heads; head h reads keys and values of head h / (q_heads / kv_heads).  d <= 128 coordinates.
  * Lengths may be 0 and 1, strides are in elements, any alignment will do (rows of whole 16 bytes, aligned to them, are
  * read fastest).
- * FS_F32: products on the fp32 matrix cores; where that takes long enough (1.5e9 operations, the backward pass counted 2.5 times),
+ * FS_F32: products on the fp32 matrix cores; where that takes long enough (2e9 operations forward),
  * from operands in two fp16 pieces, 22 bits of every element down to 2^-17 of its head's largest and 2^-40 of that below, summed in
  * fp32.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
  * probabilities (2^-9 of each) and their gradients are rounded to bf16 where they enter a second product.  Maxima, sums

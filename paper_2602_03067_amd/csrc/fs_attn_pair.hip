@@ -166,14 +166,16 @@ int64_t image_bytes(const AttnCall &a, int tensor)
 
 }  // namespace
 
-// The two passes and the pieces' way through memory take some 12 us; the products on the fp32 matrix cores run at 90 to 100 TFLOP/s, those
-// of pairs at several times that.  A few rows, bound by memory, gain nothing.
+// The two passes and the pieces' way through memory take 8 to 15 us.  Forward and backward, pairs and fp32 matrix cores (us, sets of
+// heads x rows x keys, d): 8 x 512 x 512, 64 (0.5e9 operations forward): 21 and 20, 52 and 56; 4 x 1024 x 1024, 64 (1.1e9): 25 and 24,
+// 57 and 64; 8 x 1024 x 1024, 64 (2.1e9): 36 and 39, 64 and 97; 8 x 4096 x 4096, 64 (34e9): 153 and 343, 430 and 1010.  A few rows,
+// bound by memory, gain nothing.
 bool pair_worth(const Ctx *c, const AttnCall &a, bool grad)
 {
     const int64_t rows = (int64_t)a.n * a.group;
     if (rows == 0 || a.m == 0 || (int64_t)a.batch * a.kv_heads > 65535) return false;
     if (c->dbg_attn_pairs) return c->dbg_attn_pairs == 1;
-    return rows > 32 && (grad ? 2.5 : 1.0) * 4.0 * (double)a.batch * a.kv_heads * rows * a.m * a.d * (a.causal ? 0.5 : 1.0) >= 1.5e9;
+    return rows > 32 && 4.0 * (double)a.batch * a.kv_heads * rows * a.m * a.d * (a.causal ? 0.5 : 1.0) >= (grad ? 0.4e9 : 2.0e9);
 }
 
 size_t pair_bytes(const AttnCall &a, bool grad)
