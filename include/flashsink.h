@@ -422,7 +422,7 @@ fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, floa
 
 /*
  * Gradients of fs_attention for the gradient d_o of its output: dq, dk, dv (q's, k's and v's shapes, all written; summed
- * over the heads that share keys), and dbias [batch][k_rows] of `dtype` (stride dbias_ld >= k_rows), NULL to skip.  o and
+ * over the heads that share keys), and dbias [batch][k_rows] of `dtype` (stride dbias_ld >= k_rows, at most 65535 sets), NULL to skip.  o and
  * stat are what fs_attention gave.  The probabilities are computed anew from stat; no n x m matrix is stored.
  */
 fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, const float *stat /* device */, const fs_heads *d_o,

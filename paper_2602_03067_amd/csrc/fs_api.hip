@@ -1464,6 +1464,7 @@ fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o,
         return st;
     if (dbias) {
         if (!attn->bias) return fail(c, FS_ERR_INVALID_ARG, "dbias without bias");
+        if (attn->batch > 65535) return fail(c, FS_ERR_BAD_SHAPE, "dbias: at most 65535 sets");
         if (attn->bias_ld == 0 && attn->batch > 1) return fail(c, FS_ERR_UNSUPPORTED, "dbias of a bias that the sets share");
         if (dbias_ld < attn->k_rows || dbias_ld > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "dbias_ld is smaller than k_rows, or beyond 2^40");
         if ((uintptr_t)dbias % k.es) return fail(c, FS_ERR_INVALID_ARG, "dbias is not aligned to its type");

@@ -226,7 +226,12 @@ template <typename T, int DP, int ROWS, int NT> struct Dma {
         const unsigned to = __builtin_amdgcn_readfirstlane(lds + (tid >> 6) * 1024);
         if (d == DP && count >= ROWS) {
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) dma16s(kAlike ? base + i * round : base, off[kAlike ? 0 : i], to + i * NT * 16);
+            for (int i = 0; i < kCount; ++i) {
+                // (a workgroup of one wave is alone with its keys: one query over 50021 keys, four sets, eight heads of d = 128,
+                // 120 us, and 130 through the caches)
+                if constexpr (NT == 64) dma16s_nt(kAlike ? base + i * round : base, off[kAlike ? 0 : i], to + i * NT * 16);
+                else dma16s(kAlike ? base + i * round : base, off[kAlike ? 0 : i], to + i * NT * 16);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < kCount; ++i)

@@ -538,15 +538,24 @@ template <typename T, int DP, bool KV> void join(Ctx *c, const AttnCall &a)
     else k_attn_grad_join<T, DP, KV, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
 }
 
+// Sum over the splits and heads that share a bias: sixteen lanes take a key each, sixteen shares side by side.
 template <typename T> __global__ __launch_bounds__(256) void k_attn_dbias(const AttnCall c)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)c.batch * c.m) return;
-    const int64_t b = at / c.m, key = at - b * c.m;
+    __shared__ float lds[16][17];
+    const int x = threadIdx.x % 16, g = threadIdx.x / 16, b = blockIdx.y, key = blockIdx.x * 16 + x;
     float acc = 0.0f;
-    for (int s = 0; s < c.splits; ++s)
-        for (int h = 0; h < c.kv_heads; ++h) acc += c.dbias_part[(((int64_t)s * c.batch + b) * c.kv_heads + h) * c.m + key];
-    ((T *)c.dbias)[b * c.dbias_ld + key] = (T)acc;
+    if (key < c.m)
+#pragma unroll 4
+        for (int i = g; i < c.splits * c.kv_heads; i += 16) {
+            const int s = i / c.kv_heads, h = i - s * c.kv_heads;
+            acc += c.dbias_part[(((int64_t)s * c.batch + b) * c.kv_heads + h) * c.m + key];
+        }
+    lds[g][x] = acc;
+    __syncthreads();
+    if (g == 0 && key < c.m) {
+        for (int i = 1; i < 16; ++i) acc += lds[i][x];
+        ((T *)c.dbias)[b * c.dbias_ld + key] = (T)acc;
+    }
 }
 
 template <typename T, int DP>
@@ -596,7 +605,7 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
             else k_attn_dkv<T, DP, RT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
         if (a.splits > 1) join<E, DP, true>(c, a);
-        if (a.dbias) k_attn_dbias<E><<<(unsigned)ceil_div((int64_t)a.batch * a.m, 256), 256, 0, c->stream>>>(a);
+        if (a.dbias) k_attn_dbias<E><<<dim3((unsigned)ceil_div(a.m, 16), (unsigned)a.batch), 256, 0, c->stream>>>(a);
     }
     FS_HIP(c, hipGetLastError());
     return FS_OK;

@@ -53,6 +53,12 @@ __device__ inline void dma16s(const void *g_uniform, unsigned lane_off, unsigned
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(g_uniform), "s"(lds_off)
                  : "memory", "m0");
 }
+// ... of what is read once only: past the caches
+__device__ inline void dma16s_nt(const void *g_uniform, unsigned lane_off, unsigned lds_off)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(lane_off), "s"(g_uniform), "s"(lds_off)
+                 : "memory", "m0");
+}
 __device__ inline void dma4s(const void *g_uniform, unsigned lane_off, unsigned lds_off)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(g_uniform), "s"(lds_off)
