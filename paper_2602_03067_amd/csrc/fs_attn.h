@@ -381,7 +381,7 @@ fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad, bool aligned);
 
 // how a forward pass is launched
 struct AttnPlan {
-    int waves, splits;
+    int rows, splits;   // packed rows of a workgroup
     bool pairs;
     int64_t grid;
     size_t part_bytes, stat_bytes, pair_bytes;

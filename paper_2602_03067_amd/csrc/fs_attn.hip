@@ -18,39 +18,46 @@ constexpr float kLog2eF = 1.44269504088896340736f;
 constexpr float kSlack = 30.0f;
 constexpr float kSlackPair = 11.0f;   // (kPairP times a probability is an fp16)
 
+// keys of a tile where a workgroup has 64 rows: 32 or 64 for each of four parts, at most 128 KB of LDS
+constexpr int few_keys(int dp) { return dp > 64 ? 128 : 256; }
+
 // waves per SIMD: what registers allow without spills
 template <typename T> constexpr int min_waves(int dp) { return std::is_same<T, float>::value && dp >= 96 ? 1 : 2; }
 
-template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD>
-__global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const AttnCall c)
+// A workgroup has RW KS waves: wave w holds the w % RW-th 32 rows of the workgroup, and takes the w / RW-th part of every tile of KTS
+// keys.  With KS > 1 the parts of a row meet in LDS at the end.
+template <typename T, int DP, int KTS, int RW, int KS, bool BIAS, Load LOAD>
+__global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const AttnCall c)
 {
     using M = Mma<T>;
     using E = typename M::Elem;
     using Frag = typename M::Frag;
     using TL = Tile<T, DP>;
-    using D = Dma<T, DP, KT, 64 * WAVES>;
+    using D = Dma<T, DP, KTS, 64 * RW * KS>;
     constexpr bool ALN = LOAD != kAny, kPair = std::is_same<T, Pair>::value, kDirect = kPair || LOAD == kDma;
-    constexpr int NT = 64 * WAVES, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
+    constexpr int KT = KTS / KS, NT = 64 * RW * KS, NS = DP / M::kStep, NB = KT / 32, NF = 32 / M::kStep, ND = DP / 32;
     constexpr int kTile = D::kTile, NPC = D::kCount;
-    static_assert(KT * TL::kPieces % NT == 0 && (!kPair || WAVES == 4), "");
+    static_assert(KTS * TL::kPieces % NT == 0 && (!kPair || RW == 4), "");
+    static_assert((KS - 1) * RW * 64 * (16 * ND + 3) * 4 <= 4 * kTile, "");
     __shared__ __align__(16) char lds[4 * kTile];
-    __shared__ __align__(16) float lbias[2][BIAS ? KT : 1];
+    __shared__ __align__(16) float lbias[2][BIAS ? KTS : 1];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-    const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
+    const int tid = threadIdx.x, lane = tid & 63, wave = KS == 1 ? tid >> 6 : (tid >> 6) % RW, part_id = KS == 1 ? 0 : (tid >> 6) / RW,
+              half = lane >> 5;
+    const int rows = c.n * c.group, blocks = (rows + 32 * RW - 1) / (32 * RW);
     const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
     const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
     const int q_len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
-    const int r = blk * 32 * WAVES + wave * 32 + (lane & 31);
+    const int r = blk * 32 * RW + wave * 32 + (lane & 31);
     const Packed pk = unpack(r, c.group);
     const bool live = r < rows && pk.q < q_len;
     // keys that this row sees: 0 .. limit - 1
     const int limit = !live ? 0 : c.causal ? min(k_len, max(0, pk.q + k_len - q_len + 1)) : k_len;
-    const int last_q = min((min(rows, (blk + 1) * 32 * WAVES) - 1) / c.group, q_len - 1);
-    const int hi = last_q < blk * 32 * WAVES / c.group ? 0 : c.causal ? min(k_len, max(0, last_q + k_len - q_len + 1)) : k_len;
-    const int tiles = (hi + KT - 1) / KT, per = (tiles + c.splits - 1) / c.splits;
+    const int last_q = min((min(rows, (blk + 1) * 32 * RW) - 1) / c.group, q_len - 1);
+    const int hi = last_q < blk * 32 * RW / c.group ? 0 : c.causal ? min(k_len, max(0, last_q + k_len - q_len + 1)) : k_len;
+    const int tiles = (hi + KTS - 1) / KTS, per = (tiles + c.splits - 1) / c.splits;
     const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
 
     const E *kp = (const E *)c.k + b * c.sk.batch + hk * c.sk.head;
@@ -72,30 +79,30 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
             ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(E) + D::piece(tid, i) * 16);
             vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(E) + D::piece(tid, i) * 16);
         }
-        if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KT, t1 - t0);
+        if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KTS, t1 - t0);
     }
     // kDma: the whole way; otherwise to registers
     auto fetch = [&](int tile, int buf) {
         if constexpr (kPair) {
-            const int64_t at = (bh * pair_rows(c.m) + (int64_t)tile * KT) * TL::kRow;
+            const int64_t at = (bh * pair_rows(c.m) + (int64_t)tile * KTS) * TL::kRow;
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            DmaImage<DP, KT, NT>::load(c.pair.img[kPairK] + at, to, tid);
-            DmaImage<DP, KT, NT>::load(c.pair.img[kPairV] + at, to + kTile, tid);
+            DmaImage<DP, KTS, NT>::load(c.pair.img[kPairK] + at, to, tid);
+            DmaImage<DP, KTS, NT>::load(c.pair.img[kPairV] + at, to + kTile, tid);
         } else if constexpr (LOAD == kDma) {
-            const char *kb = (const char *)(kp + (int64_t)tile * KT * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KT * c.sv.row);
+            const char *kb = (const char *)(kp + (int64_t)tile * KTS * c.sk.row), *vb = (const char *)(vp + (int64_t)tile * KTS * c.sv.row);
             const unsigned to = lds_address(base) + 2 * buf * kTile;
-            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(E), to, tid, c.d, k_len - tile * KT);
-            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(E), to + kTile, tid, c.d, k_len - tile * KT);
+            D::load(kb, ko, D::kRound * c.sk.row * (int)sizeof(E), to, tid, c.d, k_len - tile * KTS);
+            D::load(vb, vo, D::kRound * c.sv.row * (int)sizeof(E), to + kTile, tid, c.d, k_len - tile * KTS);
         } else {
 #pragma unroll
             for (int i = 0; i < NPC; ++i) {
-                const int p = tid + i * NT, pc = p % TL::kPieces, key = tile * KT + p / TL::kPieces, at = min(key, k_len - 1);
+                const int p = tid + i * NT, pc = p % TL::kPieces, key = tile * KTS + p / TL::kPieces, at = min(key, k_len - 1);
                 kr[i] = load_piece<E, ALN>(kp + (int64_t)at * c.sk.row, pc, c.d);
                 vr[i] = load_piece<E, ALN>(vp + (int64_t)at * c.sv.row, pc, c.d);
                 if (BIAS && bp[at] == -INFINITY) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);   // what removed keys hold does not matter
             }
         }
-        if (BIAS && tid < KT) br = bp[min(tile * KT + tid, k_len - 1)];
+        if (BIAS && tid < KTS) br = bp[min(tile * KTS + tid, k_len - 1)];
     };
     auto put = [&](int buf) {
         if constexpr (!kDirect) {
@@ -106,7 +113,7 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
                 *(uint4 *)(lds + (2 * buf + 1) * kTile + at) = vr[i];
             }
         }
-        if (BIAS && tid < KT) lbias[buf][tid] = br;
+        if (BIAS && tid < KTS) lbias[buf][tid] = br;
     };
 
     if (t0 < t1) fetch(t0, 0);
@@ -139,7 +146,7 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
     // scores of a tile; returns the row's largest
     auto scores = [&](int tile, f32x16 (&s)[NB]) {
         const int buf = (tile - t0) & 1;
-        const LdsPtr lk = base + 2 * buf * kTile;
+        const LdsPtr lk = base + 2 * buf * kTile + part_id * KT * TL::kRow;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             s[nb] = (f32x16)(0.0f);
@@ -151,13 +158,14 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * g + 4 * half];
+                    const f32x4 add = *(const f32x4 *)&lbias[buf][part_id * KT + nb * 32 + 8 * g + 4 * half];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s[nb][4 * g + j] = fmaf(s[nb][4 * g + j], scale, add[j]);
                 }
         }
-        if (__any(limit < (tile + 1) * KT)) {
-            const int key0 = tile * KT + 4 * half;
+        const int first = tile * KTS + part_id * KT;
+        if (__any(limit < first + KT)) {
+            const int key0 = first + 4 * half;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -173,7 +181,7 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
     };
     // their exponentials into the sum and, times the values, into the accumulators
     auto accumulate = [&](int tile, f32x16 (&s)[NB]) {
-        const LdsPtr lv = base + 2 * ((tile - t0) & 1) * kTile + kTile;
+        const LdsPtr lv = base + 2 * ((tile - t0) & 1) * kTile + kTile + part_id * KT * TL::kRow;
         const float safe = ref == -INFINITY ? 0.0f : ref, off = safe * unit - (kPair ? 4.0f : 0.0f);   // (kPairP = 2^4)
         float part = 0.0f;
 #pragma unroll
@@ -230,6 +238,30 @@ __global__ __launch_bounds__(64 * WAVES, min_waves<T>(DP)) void k_attn(const Att
     }
 
     sum = across_halves_sum(sum);
+    if constexpr (KS > 1) {   // (the last tile's barrier has passed: nobody reads keys any more)
+        float *at = (float *)lds + ((part_id - 1) * RW + wave) * (16 * ND + 3) * 64 + lane;
+        if (part_id > 0) {
+#pragma unroll
+            for (int i = 0; i < 16 * ND; ++i) at[64 * i] = o[i / 16][i % 16];
+            at[64 * 16 * ND] = top;
+            at[64 * (16 * ND + 1)] = ref;
+            at[64 * (16 * ND + 2)] = sum;
+        }
+        __syncthreads();
+        if (part_id > 0) return;
+        for (int k = 1; k < KS; ++k) {
+            const float *in = (const float *)lds + ((k - 1) * RW + wave) * (16 * ND + 3) * 64 + lane;
+            const float itop = in[64 * 16 * ND], iref = in[64 * (16 * ND + 1)], isum = in[64 * (16 * ND + 2)];
+            // below the higher of the two references (from minus infinity: nothing seen yet)
+            const float next = fmaxf(ref, iref), f = ref == next ? 1.0f : __builtin_amdgcn_exp2f((ref - next) * unit),
+                        g = iref == next ? 1.0f : __builtin_amdgcn_exp2f((iref - next) * unit);
+            top = fmaxf(top, itop);
+            ref = next;
+            sum = fmaf(isum, g, sum * f);
+#pragma unroll
+            for (int i = 0; i < 16 * ND; ++i) o[i / 16][i % 16] = fmaf(in[64 * i], g, o[i / 16][i % 16] * f);
+        }
+    }
     if (r >= rows) return;
     const float st = BIAS ? 1.0f : scale;   // the running values as scores
     if constexpr (kPair) {
@@ -322,25 +354,25 @@ template <typename T, int DP> void join(Ctx *c, const AttnCall &a)
     else k_attn_join<T, DP, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
 }
 
-template <typename T, int DP, int KT, int WAVES>
+template <typename T, int DP, int KTS, int RW, int KS>
 fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
 {
-    const unsigned g = (unsigned)grid, nt = 64 * WAVES;
+    const unsigned g = (unsigned)grid, nt = 64 * RW * KS;
     if constexpr (std::is_same<T, Pair>::value) {   // (rows of the tensors themselves are only written)
         if (a.bias) {
-            if (load != kAny) k_attn<T, DP, KT, WAVES, true, kVec><<<g, nt, 0, c->stream>>>(a);
-            else k_attn<T, DP, KT, WAVES, true, kAny><<<g, nt, 0, c->stream>>>(a);
+            if (load != kAny) k_attn<T, DP, KTS, RW, KS, true, kVec><<<g, nt, 0, c->stream>>>(a);
+            else k_attn<T, DP, KTS, RW, KS, true, kAny><<<g, nt, 0, c->stream>>>(a);
         } else {
-            if (load != kAny) k_attn<T, DP, KT, WAVES, false, kVec><<<g, nt, 0, c->stream>>>(a);
-            else k_attn<T, DP, KT, WAVES, false, kAny><<<g, nt, 0, c->stream>>>(a);
+            if (load != kAny) k_attn<T, DP, KTS, RW, KS, false, kVec><<<g, nt, 0, c->stream>>>(a);
+            else k_attn<T, DP, KTS, RW, KS, false, kAny><<<g, nt, 0, c->stream>>>(a);
         }
     } else if (a.bias) {
-        if (load != kAny) k_attn<T, DP, KT, WAVES, true, kVec><<<g, nt, 0, c->stream>>>(a);
-        else k_attn<T, DP, KT, WAVES, true, kAny><<<g, nt, 0, c->stream>>>(a);
+        if (load != kAny) k_attn<T, DP, KTS, RW, KS, true, kVec><<<g, nt, 0, c->stream>>>(a);
+        else k_attn<T, DP, KTS, RW, KS, true, kAny><<<g, nt, 0, c->stream>>>(a);
     } else {
-        if (load == kDma) k_attn<T, DP, KT, WAVES, false, kDma><<<g, nt, 0, c->stream>>>(a);
-        else if (load == kVec) k_attn<T, DP, KT, WAVES, false, kVec><<<g, nt, 0, c->stream>>>(a);
-        else k_attn<T, DP, KT, WAVES, false, kAny><<<g, nt, 0, c->stream>>>(a);
+        if (load == kDma) k_attn<T, DP, KTS, RW, KS, false, kDma><<<g, nt, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn<T, DP, KTS, RW, KS, false, kVec><<<g, nt, 0, c->stream>>>(a);
+        else k_attn<T, DP, KTS, RW, KS, false, kAny><<<g, nt, 0, c->stream>>>(a);
     }
     if (a.splits > 1) join<typename Mma<T>::Elem, DP>(c, a);
     FS_HIP(c, hipGetLastError());
@@ -350,31 +382,29 @@ fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
 fs_status pairs_by_width(Ctx *c, const AttnCall &a, Load load, int64_t grid)
 {
     switch ((a.d + 31) / 32) {
-    case 1: return run<Pair, 32, 64, 4>(c, a, load, grid);
-    case 2: return run<Pair, 64, 64, 4>(c, a, load, grid);
-    case 3: return run<Pair, 96, 32, 4>(c, a, load, grid);
-    default: return run<Pair, 128, 32, 4>(c, a, load, grid);
+    case 1: return run<Pair, 32, 64, 4, 1>(c, a, load, grid);
+    case 2: return run<Pair, 64, 64, 4, 1>(c, a, load, grid);
+    case 3: return run<Pair, 96, 32, 4, 1>(c, a, load, grid);
+    default: return run<Pair, 128, 32, 4, 1>(c, a, load, grid);
     }
 }
 
-template <typename T>
-fs_status by_width(Ctx *c, const AttnCall &a, Load load, int waves, int64_t grid)
+template <typename T, int DP> fs_status by_rows(Ctx *c, const AttnCall &a, Load load, const AttnPlan &p)
 {
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32;
-    const int dp = (a.d + 31) / 32;
-    if (waves == 1) {
-        switch (dp) {
-        case 1: return run<T, 32, 32, 1>(c, a, load, grid);
-        case 2: return run<T, 64, 32, 1>(c, a, load, grid);
-        case 3: return run<T, 96, 32, 1>(c, a, load, grid);
-        default: return run<T, 128, 32, 1>(c, a, load, grid);
-        }
-    }
-    switch (dp) {
-    case 1: return run<T, 32, KT, 4>(c, a, load, grid);
-    case 2: return run<T, 64, KT, 4>(c, a, load, grid);
-    case 3: return run<T, 96, KT, 4>(c, a, load, grid);
-    default: return run<T, 128, KT, 4>(c, a, load, grid);
+    constexpr bool f32 = std::is_same<T, float>::value;
+    if (p.rows == 32) return run<T, DP, 32, 1, 1>(c, a, load, p.grid);
+    if constexpr (!f32)
+        if (p.rows == 64) return run<T, DP, few_keys(DP), 2, 4>(c, a, load, p.grid);
+    return run<T, DP, f32 ? 32 : 64, 4, 1>(c, a, load, p.grid);
+}
+
+template <typename T> fs_status by_width(Ctx *c, const AttnCall &a, Load load, const AttnPlan &p)
+{
+    switch ((a.d + 31) / 32) {
+    case 1: return by_rows<T, 32>(c, a, load, p);
+    case 2: return by_rows<T, 64>(c, a, load, p);
+    case 3: return by_rows<T, 96>(c, a, load, p);
+    default: return by_rows<T, 128>(c, a, load, p);
     }
 }
 
@@ -385,11 +415,15 @@ AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
     AttnPlan p;
     const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads;
     p.pairs = f32 && pair_worth(c, a, false);
-    p.waves = rows <= 32 && !p.pairs ? 1 : 4;
-    const int kt = p.waves == 1 || f32 ? 32 : 64;
-    const int64_t blocks = ceil_div(rows, 32 * p.waves) * heads, tiles = ceil_div(a.m, kt);
-    const int64_t want = (int64_t)c->num_cu * (p.waves == 1 ? 4 : 2);
-    p.splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(blocks, 1), tiles / 4));
+    // Rows of a workgroup: 128, or, in bf16 where these do not fill the chip, 64 whose keys eight waves share (16 heads of 1024 points,
+    // d = 64: 14.5 us; four splits of 128 rows and their merge take 21; float32 in 64-row workgroups is slower), or 32 of one wave for
+    // a few queries over long keys, which is bound by memory.
+    const int64_t wide = ceil_div(rows, 128) * heads, few = few_keys((int)round_up(a.d, 32));
+    p.rows = p.pairs ? 128 : rows <= 32 ? 32 : !f32 && wide < c->num_cu && a.m >= few ? 64 : 128;
+    const int64_t kt = p.rows == 64 ? few : p.rows == 32 || f32 ? 32 : 64;
+    const int64_t blocks = ceil_div(rows, p.rows) * heads, tiles = ceil_div(a.m, kt);
+    const int64_t want = (int64_t)c->num_cu * (p.rows == 32 ? 4 : p.rows == 64 ? 1 : 2);
+    p.splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(blocks, 1), tiles / (p.rows == 64 ? 2 : 4)));
     p.grid = blocks * p.splits;
     const int64_t dp = round_up(a.d, 32), total = heads * rows * p.splits;
     p.part_bytes = p.splits > 1 ? (size_t)total * dp * 4 : 0;
@@ -407,7 +441,7 @@ fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bo
         const fs_status st = launch_pairs(c, a, false, aligned);
         return st ? st : pairs_by_width(c, a, load, p.grid);
     }
-    return f32 ? by_width<float>(c, a, load, p.waves, p.grid) : by_width<__bf16>(c, a, load, p.waves, p.grid);
+    return f32 ? by_width<float>(c, a, load, p) : by_width<__bf16>(c, a, load, p);
 }
 
 }  // namespace fs
