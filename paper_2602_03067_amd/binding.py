@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import os
+import struct
 from typing import Optional, Tuple
 
 import numpy as np
@@ -111,9 +112,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fs_grad_x.argtypes = [vp, PP, f32, vp, vp, i32, vp, i64]
     lib.fs_grad_y.argtypes = [vp, PP, f32, vp, vp, i32, vp, i64]
     lib.fs_hvp.argtypes = [vp, PP, f32, vp, vp, vp, i64, f32, f32, i32, vp, i64, ctypes.POINTER(i32)]
-    PH = ctypes.POINTER(FsHeads)
-    lib.fs_attention.argtypes = [vp, ctypes.POINTER(FsAttn), PH, vp]
-    lib.fs_attention_grad.argtypes = [vp, ctypes.POINTER(FsAttn), PH, vp, PH, PH, PH, PH, vp, i64]
+    # (fs_attn and fs_heads as bytes or by reference)
+    lib.fs_attention.argtypes = [vp, vp, vp, vp]
+    lib.fs_attention_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64]
     lib.fs_layer_norm.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i32, f32, vp, i64, vp]
     lib.fs_layer_norm_grad.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, vp, vp, i64, vp, i64, vp, vp]
     lib.fs_adamw.argtypes = [vp, ctypes.POINTER(FsAdamwArgs), ctypes.POINTER(FsAdamwTensor), i32]
@@ -149,38 +150,44 @@ _get_dtype, _get_is_cuda = operator.attrgetter("dtype"), operator.attrgetter("is
 _DTYPES = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
 
 
-def _heads(t: torch.Tensor, name: str, shape, dtype) -> FsHeads:
-    """The C view of a (sets, rows, heads, coordinates) tensor."""
-    if not t.is_cuda or t.dtype != dtype:
+def _heads(t: torch.Tensor, name: str, shape, dtype):
+    """Address and strides of a (sets, rows, heads, coordinates) tensor, as fs_heads has them."""
+    if t.dtype is not dtype or not t.is_cuda:
         raise TypeError("%s must be a %s tensor on the GPU" % (name, dtype))
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     b, r, h, e = t.stride()
     if e != 1 and shape[3] != 1:
         raise ValueError("%s must have unit stride within a head" % name)
-    return FsHeads(t.data_ptr(), b, r, h)
+    return t.data_ptr(), b, r, h
+
+
+# (the structures' bytes: made faster than ctypes fills their fields)
+_HEADS, _ATTN = struct.Struct("Qqqq"), struct.Struct("QqqqQqqqQqqqiiqqqqqqf4xQQQq")
+assert _HEADS.size == ctypes.sizeof(FsHeads) and _ATTN.size == ctypes.sizeof(FsAttn)
 
 
 def _lengths(t: Optional[torch.Tensor], name: str, batch: int):
     if t is None:
-        return None
+        return 0
     if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.shape != (batch,):
         raise TypeError("%s must be a contiguous int32 GPU tensor of %d lengths" % (name, batch))
     return t.data_ptr()
 
 
-def _attn(q, k, v, scale, causal, q_len, k_len, bias) -> FsAttn:
-    if q.dim() != 4 or k.dim() != 4 or q.dtype not in _DTYPES:
+def _attn(q, k, v, scale, causal, q_len, k_len, bias):
+    dtype = q.dtype
+    if q.dim() != 4 or k.dim() != 4 or dtype not in _DTYPES:
         raise TypeError("q, k, v must be float32 or bfloat16 tensors of (sets, rows, heads, coordinates)")
     (batch, n, heads, d), (_, m, kv_heads, _) = q.shape, k.shape
-    a = FsAttn(_heads(q, "q", q.shape, q.dtype), _heads(k, "k", (batch, m, kv_heads, d), q.dtype),
-               _heads(v, "v", (batch, m, kv_heads, d), q.dtype), _DTYPES[q.dtype], 1 if causal else 0, batch, n, m, heads, kv_heads, d,
-               d ** -0.5 if scale is None else scale, _lengths(q_len, "q_len", batch), _lengths(k_len, "k_len", batch), None, 0)
+    kv, at, ld = (batch, m, kv_heads, d), 0, 0
     if bias is not None:
         if not bias.is_cuda or bias.dtype != torch.float32 or bias.shape != (batch, m) or (m > 1 and bias.stride(1) != 1):
             raise TypeError("bias must be a float32 GPU tensor of (sets, keys) with unit inner stride")
-        a.bias, a.bias_ld = bias.data_ptr(), bias.stride(0) if batch > 1 else m
-    return a
+        at, ld = bias.data_ptr(), bias.stride(0) if batch > 1 else m
+    return _ATTN.pack(*_heads(q, "q", q.shape, dtype), *_heads(k, "k", kv, dtype), *_heads(v, "v", kv, dtype), _DTYPES[dtype], 1 if causal else 0,
+                      batch, n, m, heads, kv_heads, d, d ** -0.5 if scale is None else scale, _lengths(q_len, "q_len", batch),
+                      _lengths(k_len, "k_len", batch), at, ld)
 
 
 def _matrix(t: torch.Tensor, name: str):
@@ -440,9 +447,9 @@ class Context:
         ``scale`` defaults to d^-1/2, ``bias`` (sets, keys) is added to the scores (log-weights; -inf removes a key), ``q_len``,
         ``k_len`` are the lengths of padded sets.  ``stat`` is what ``fs_attention_grad`` takes up."""
         a = _attn(q, k, v, scale, causal, q_len, k_len, bias)
-        o, stat = q.new_empty(q.shape), q.new_empty((a.batch, a.q_heads, a.q_rows, 2), dtype=torch.float32)
-        self._check(self.lib.fs_attention(self.h, ctypes.byref(a), ctypes.byref(_heads(o, "o", q.shape, q.dtype)), stat.data_ptr()),
-                    "fs_attention")
+        b, n, h, _ = shape = q.shape
+        o, stat = q.new_empty(shape), q.new_empty((b, h, n, 2), dtype=torch.float32)
+        self._check(self.lib.fs_attention(self.h, a, _HEADS.pack(*_heads(o, "o", shape, q.dtype)), stat.data_ptr()), "fs_attention")
         return o, stat
 
     def fs_attention_grad(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, stat: torch.Tensor, do: torch.Tensor,
@@ -451,15 +458,16 @@ class Context:
         """Gradients of ``fs_attention`` (same mask arguments) for the gradient ``do`` of its output: (dq, dk, dv), with ``want_bias``
         (dq, dk, dv, dbias)."""
         a = _attn(q, k, v, scale, causal, q_len, k_len, bias)
-        _dev_f32(stat, "stat", (a.batch, a.q_heads, a.q_rows, 2))
+        shape, dtype = q.shape, q.dtype
+        _dev_f32(stat, "stat", (shape[0], shape[2], shape[1], 2))
         if want_bias and bias is None:
             raise ValueError("want_bias without a bias")
         g = [q.new_empty(t.shape) for t in (q, k, v)]
         db = q.new_empty(bias.shape) if want_bias else None
-        h = [ctypes.byref(_heads(t, nm, s, q.dtype)) for t, nm, s in
-             ((o, "o", q.shape), (do, "do", q.shape), (g[0], "dq", q.shape), (g[1], "dk", k.shape), (g[2], "dv", k.shape))]
-        self._check(self.lib.fs_attention_grad(self.h, ctypes.byref(a), h[0], stat.data_ptr(), h[1], h[2], h[3], h[4],
-                                               None if db is None else db.data_ptr(), a.k_rows), "fs_attention_grad")
+        h = [_HEADS.pack(*_heads(t, nm, sh, dtype)) for t, nm, sh in
+             ((o, "o", shape), (do, "do", shape), (g[0], "dq", shape), (g[1], "dk", k.shape), (g[2], "dv", k.shape))]
+        self._check(self.lib.fs_attention_grad(self.h, a, h[0], stat.data_ptr(), h[1], h[2], h[3], h[4],
+                                               None if db is None else db.data_ptr(), k.shape[1]), "fs_attention_grad")
         return (*g, db) if want_bias else tuple(g)
 
     def fs_layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5):
