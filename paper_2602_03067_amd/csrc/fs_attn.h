@@ -346,26 +346,35 @@ __device__ inline Packed unpack(int r, int group)
 // What a workgroup works on.  Workgroups that share an XCD's L2 (ids equal mod 8) take consecutive work of the order (set and kv head;
 // block of rows or keys; split).  Under a causal line blocks are of unequal length, and consecutive blocks would give one XCD the
 // long half of a head and its neighbour the short one: `rank` counts blocks from the longest, and
-//  - where every XCD has whole heads, blocks come by rank, the longest first;
+//  - where every XCD has whole heads, their blocks come by rank, the longest of all heads first;
 //  - where a head has a whole number of XCDs, each takes every so many-th of them;
-//  - otherwise they alternate between long and short ones.
+//  - otherwise the longest of all heads come first everywhere, and XCDs share heads.
 struct Work {
     int split, rank, hk, b;
 };
 __device__ inline Work work_of(int id, int total, int splits, int blocks, int kv_heads, bool causal)
 {
-    const int x = id & 7, per = total >> 3, more = total & 7;
-    id = x * per + (x < more ? x : more) + (id >> 3);
+    const int x = id & 7, per = total >> 3, more = total & 7, heads = total / (splits * blocks);
+    const int share = heads < 8 && 8 % heads == 0 && blocks % (8 / heads) == 0 ? 8 / heads : 0;   // XCDs of a head
+    const bool mixed = causal && heads % 8 != 0 && !share;
+    if (!mixed) id = x * per + (x < more ? x : more) + (id >> 3);
     Work w;
     w.split = id % splits;
     id /= splits;
-    int j = id % blocks;
-    id /= blocks;
-    const int heads = total / (splits * blocks);
-    if (causal && heads % 8 != 0) {
-        const int share = heads < 8 && 8 % heads == 0 ? 8 / heads : 0;
-        if (share && blocks % share == 0) j = j % (blocks / share) * share + j / (blocks / share);
-        else j = j & 1 ? blocks - 1 - j / 2 : j / 2;
+    int j;
+    if (mixed) {
+        j = id / heads;
+        id %= heads;
+    } else {
+        j = id % blocks;
+        id /= blocks;
+        if (causal && share) {
+            j = j % (blocks / share) * share + j / (blocks / share);
+        } else if (causal) {
+            const int own = heads / 8, at = id % own * blocks + j;   // heads of an XCD; place in its order
+            j = at / own;
+            id += at % own - id % own;
+        }
     }
     w.rank = j;
     w.hk = id % kv_heads;
