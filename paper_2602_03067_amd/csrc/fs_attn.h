@@ -348,15 +348,16 @@ __device__ inline Packed unpack(int r, int group)
 // long half of a head and its neighbour the short one: `rank` counts blocks from the longest, and
 //  - where every XCD has whole heads, their blocks come by rank, the longest of all heads first;
 //  - where a head has a whole number of XCDs, each takes every so many-th of them;
-//  - otherwise the longest of all heads come first everywhere, and XCDs share heads.
+//  - otherwise the longest of all heads come first everywhere, and XCDs share heads;
+// the last also where sets have lengths of their own: an XCD with the longest sets alone would finish after the others.
 struct Work {
     int split, rank, hk, b;
 };
-__device__ inline Work work_of(int id, int total, int splits, int blocks, int kv_heads, bool causal)
+__device__ inline Work work_of(int id, int total, int splits, int blocks, int kv_heads, bool causal, bool ragged)
 {
     const int x = id & 7, per = total >> 3, more = total & 7, heads = total / (splits * blocks);
     const int share = heads < 8 && 8 % heads == 0 && blocks % (8 / heads) == 0 ? 8 / heads : 0;   // XCDs of a head
-    const bool mixed = causal && heads % 8 != 0 && !share;
+    const bool mixed = ragged || (causal && heads % 8 != 0 && !share);
     if (!mixed) id = x * per + (x < more ? x : more) + (id >> 3);
     Work w;
     w.split = id % splits;

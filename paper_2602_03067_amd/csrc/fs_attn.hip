@@ -45,7 +45,7 @@ __global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const A
     const int tid = threadIdx.x, lane = tid & 63, wave = KS == 1 ? tid >> 6 : (tid >> 6) % RW, part_id = KS == 1 ? 0 : (tid >> 6) / RW,
               half = lane >> 5;
     const int rows = c.n * c.group, blocks = (rows + 32 * RW - 1) / (32 * RW);
-    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.k_len || c.q_len);
     const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
-    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.k_len || c.q_len);
     const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves<T>(DP)) void k_attn_dkv(const
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (c.m + 32 * WAVES - 1) / (32 * WAVES);
-    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal);
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.k_len || c.q_len);
     const int split = w.split, blk = w.rank, hk = w.hk, b = w.b;
     const int64_t bh = (int64_t)b * c.kv_heads + hk;
 
