@@ -45,7 +45,7 @@ __global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const A
     const int tid = threadIdx.x, lane = tid & 63, wave = KS == 1 ? tid >> 6 : (tid >> 6) % RW, part_id = KS == 1 ? 0 : (tid >> 6) / RW,
               half = lane >> 5;
     const int rows = c.n * c.group, blocks = (rows + 32 * RW - 1) / (32 * RW);
-    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.k_len || c.q_len);
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.batch > 1 && (c.k_len || c.q_len));
     const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
@@ -139,10 +139,15 @@ __global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const A
     float ref = -INFINITY, top = -INFINITY, sum = 0.0f;
     const typename TL::Lanes ln = TL::lanes(lane);
 
+    constexpr bool kRemoved = BIAS && !kPair && LOAD == kDma;
+    auto removed = [&](int buf) {
+        if constexpr (kRemoved) clear_removed<T, DP, KTS, NT>(lds + 2 * buf * kTile, lds + (2 * buf + 1) * kTile, lbias[buf], tid);
+    };
     if (t0 < t1) put(0);
     dma_wait();   // (of q as well: not inside the loop, where it would wait for the next tile)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
+    if (kRemoved && t0 < t1) removed(0);
     // scores of a tile; returns the row's largest
     auto scores = [&](int tile, f32x16 (&s)[NB]) {
         const int buf = (tile - t0) & 1;
@@ -208,6 +213,7 @@ __global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const A
         if ((!kDirect || BIAS) && tile + 1 < t1) put((tile + 1 - t0) & 1);
         if (kDirect) dma_wait();
         __syncthreads();
+        if (kRemoved && tile + 1 < t1) removed((tile + 1 - t0) & 1);
     };
     int tile = t0;
     bool fetched = false;
@@ -367,7 +373,8 @@ fs_status run(Ctx *c, const AttnCall &a, Load load, int64_t grid)
             else k_attn<T, DP, KTS, RW, KS, false, kAny><<<g, nt, 0, c->stream>>>(a);
         }
     } else if (a.bias) {
-        if (load != kAny) k_attn<T, DP, KTS, RW, KS, true, kVec><<<g, nt, 0, c->stream>>>(a);
+        if (load == kDma) k_attn<T, DP, KTS, RW, KS, true, kDma><<<g, nt, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn<T, DP, KTS, RW, KS, true, kVec><<<g, nt, 0, c->stream>>>(a);
         else k_attn<T, DP, KTS, RW, KS, true, kAny><<<g, nt, 0, c->stream>>>(a);
     } else {
         if (load == kDma) k_attn<T, DP, KTS, RW, KS, false, kDma><<<g, nt, 0, c->stream>>>(a);

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (rows + 32 * WAVES - 1) / (32 * WAVES);
-    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.k_len || c.q_len);
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.batch > 1 && (c.k_len || c.q_len));
     const int split = w.split, blk = blocks - 1 - w.rank, hk = w.hk, b = w.b;
 
     const int k_len = c.k_len ? min(max(c.k_len[b], 0), c.m) : c.m;
@@ -173,10 +173,15 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     f32x16 dq[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) dq[i] = (f32x16)(0.0f);
+    constexpr bool kRemoved = BIAS && !kPair && LOAD == kDma;
+    auto removed = [&](int buf) {
+        if constexpr (kRemoved) clear_removed<T, DP, KT, NT>(lds + 2 * buf * kTile, lds + (2 * buf + 1) * kTile, lbias[buf], tid);
+    };
     if (t0 < t1) put(0);
     dma_wait();
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
+    if (kRemoved && t0 < t1) removed(0);
     for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
         const LdsPtr lk = base + 2 * buf * kTile, lv = lk + kTile;
@@ -220,6 +225,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
         if ((!kDirect || BIAS) && tile + 1 < t1) put(buf ^ 1);
         if (kDirect) dma_wait();
         __syncthreads();
+        if (kRemoved && tile + 1 < t1) removed(buf ^ 1);
     }
     if (r >= rows) return;
     if constexpr (kPair) {
@@ -259,7 +265,7 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves<T>(DP)) void k_attn_dkv(const
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int rows = c.n * c.group, blocks = (c.m + 32 * WAVES - 1) / (32 * WAVES);
-    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.k_len || c.q_len);
+    const Work w = work_of(blockIdx.x, gridDim.x, c.splits, blocks, c.kv_heads, c.causal, c.batch > 1 && (c.k_len || c.q_len));
     const int split = w.split, blk = w.rank, hk = w.hk, b = w.b;
     const int64_t bh = (int64_t)b * c.kv_heads + hk;
 
@@ -562,7 +568,7 @@ template <typename T, int DP>
 fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Load rows_load)
 {
     using E = typename Mma<T>::Elem;
-    constexpr bool kPair = std::is_same<T, Pair>::value;
+    constexpr Load kBest = std::is_same<T, Pair>::value ? kVec : kDma;   // (of pairs only their images are direct)
     constexpr int RT = row_tile<T>(DP), KT = RT;
     Arena A;
     a.row_stat = (float *)(ws + A.take(p.stat_bytes));
@@ -573,14 +579,12 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
     if (p.q_grid) {
         const unsigned grid = (unsigned)p.q_grid;
         if (a.bias) {
-            if (keys != kAny) k_attn_dq<T, DP, KT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if (keys == kDma) k_attn_dq<T, DP, KT, 4, true, kBest><<<grid, 256, 0, c->stream>>>(a);
+            else if (keys == kVec) k_attn_dq<T, DP, KT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dq<T, DP, KT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
         } else {
-            if constexpr (!kPair) {
-                if (keys == kDma) k_attn_dq<T, DP, KT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
-            }
-            if (keys == kDma && !kPair) {
-            } else if (keys != kAny) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if (keys == kDma) k_attn_dq<T, DP, KT, 4, false, kBest><<<grid, 256, 0, c->stream>>>(a);
+            else if (keys == kVec) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dq<T, DP, KT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
         if (a.splits > 1) join<E, DP, false>(c, a);
@@ -590,18 +594,12 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
     if (p.k_grid) {
         const unsigned grid = (unsigned)p.k_grid;
         if (a.bias) {
-            if constexpr (!kPair) {
-                if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, true, kDma><<<grid, 256, 0, c->stream>>>(a);
-            }
-            if (rows_load == kDma && !kPair) {
-            } else if (rows_load != kAny) k_attn_dkv<T, DP, RT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, true, kBest><<<grid, 256, 0, c->stream>>>(a);
+            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dkv<T, DP, RT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
         } else {
-            if constexpr (!kPair) {
-                if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, false, kDma><<<grid, 256, 0, c->stream>>>(a);
-            }
-            if (rows_load == kDma && !kPair) {
-            } else if (rows_load != kAny) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
+            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, false, kBest><<<grid, 256, 0, c->stream>>>(a);
+            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
             else k_attn_dkv<T, DP, RT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
         }
         if (a.splits > 1) join<E, DP, true>(c, a);
