@@ -441,8 +441,8 @@ AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
 
 fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bool aligned)
 {
-    // (offsets of 64 rows in 32 bits)
-    const int64_t most = std::max(a.sk.row, a.sv.row) * (f32 ? 4 : 2) * 64;
+    // (direct loads: offsets of 128 rows in 32 bits, as many as a round of eight waves or a tile of d = 96 has)
+    const int64_t most = std::max(a.sk.row, a.sv.row) * (f32 ? 4 : 2) * 128;
     const Load load = !aligned ? kAny : most < (int64_t(1) << 31) ? kDma : kVec;
     if (p.pairs) {
         const fs_status st = launch_pairs(c, a, false, aligned);
