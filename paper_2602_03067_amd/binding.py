@@ -529,7 +529,8 @@ class AdamW:
     """AdamW over many tensors in one call of the library (``fs_adamw``): the weights are updated in place.
 
     ``state_bits`` 8 keeps m and sqrt(v) as float8 codes under a scale for every 256 weights.  ``master``: float copies of bf16
-    weights.  The state is made here unless it is given (``m``, ``v``, ``m_scale``, ``v_scale``, and ``step``, the steps already taken).
+    weights.  The state is made here unless it is given (``m``, ``v``, ``m_scale``, ``v_scale``, and ``step``, the steps already taken);
+    its tensors and the master copies stay the ones of the beginning: another state is copied into them.
     """
 
     def __init__(self, ctx: Context, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
@@ -555,9 +556,7 @@ class AdamW:
                     raise TypeError("a state tensor does not fit its weights")
             return list(given)
 
-        for p in self.params:
-            if not p.is_cuda or p.dtype != self.p_dtype or not p.is_contiguous():
-                raise TypeError("weights must be contiguous GPU tensors of one type")
+        self._check_params()
         self.m = made(m, kind, lambda p: p.numel(), 0.0)
         self.v = made(v, kind, lambda p: p.numel(), 0.0)
         self.m_scale = self.v_scale = self.master = None
@@ -571,11 +570,17 @@ class AdamW:
         for tensors, field in lists:
             for entry, t in zip(self._table, tensors or ()):
                 setattr(entry, field, t.data_ptr())
-        for entry, p in zip(self._table, self.params):
-            entry.n = p.numel()
         self._sizes = [p.numel() for p in self.params]
-        self._at = np.frombuffer(self._table, dtype=np.int64).reshape(len(self.params), 8)   # (the table's addresses; g is the second)
+        for entry, n in zip(self._table, self._sizes):
+            entry.n = n
+        self._at = np.frombuffer(self._table, dtype=np.int64).reshape(len(self.params), 8)   # (the table's addresses: p, g, ...)
+        self._p_at = list(map(torch.Tensor.data_ptr, self.params))
         self._args = FsAdamwArgs(p_dtype=_DTYPES[self.p_dtype], state_bits=state_bits)
+
+    def _check_params(self):
+        for p in self.params:
+            if not p.is_cuda or p.dtype != self.p_dtype or not p.is_contiguous():
+                raise TypeError("weights must be contiguous GPU tensors of one type")
 
     def step(self, grads, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step with these gradients (one type, contiguous, in the order of the weights).  ``grad_scale``: a float32 GPU scalar
@@ -590,6 +595,13 @@ class AdamW:
                 or not all(map(torch.Tensor.is_contiguous, grads))):
             raise TypeError("a gradient does not fit its weights")
         self._at[:, 1] = list(map(torch.Tensor.data_ptr, grads))
+        p_at = list(map(torch.Tensor.data_ptr, self.params))
+        if p_at != self._p_at:   # a weight was given other memory
+            self._check_params()
+            if list(map(torch.Tensor.numel, self.params)) != self._sizes:
+                raise ValueError("a weight changed its size")
+            self._p_at = p_at
+            self._at[:, 0] = p_at
         a = self._args
         a.lr, (a.beta1, a.beta2), a.eps, a.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
         a.step, a.g_dtype = self.step_count + 1, _DTYPES[kind]
