@@ -166,16 +166,18 @@ int64_t image_bytes(const AttnCall &a, int tensor)
 
 }  // namespace
 
-// The two passes and the pieces' way through memory take 8 to 15 us.  Forward and backward, pairs and fp32 matrix cores (us, sets of
-// heads x rows x keys, d): 8 x 512 x 512, 64 (0.5e9 operations forward): 21 and 20, 52 and 56; 4 x 1024 x 1024, 64 (1.1e9): 25 and 24,
-// 57 and 64; 8 x 1024 x 1024, 64 (2.1e9): 36 and 39, 64 and 97; 8 x 4096 x 4096, 64 (34e9): 153 and 343, 430 and 1010.  A few rows,
-// bound by memory, gain nothing.
+// The two passes and the pieces' way through memory take 8 to 15 us.  What they save grows with the products, which are padded to 32
+// coordinates.  Pairs and fp32 matrix cores, us (heads x rows x keys, d, padded operations forward), forward: 16 x 500 x 500, 64 (1.0e9)
+// 27.0 and 23.0; 8 x 600 x 600, 96 (1.1e9) 29.4 and 30.1; 4 x 800 x 800, 128 (1.3e9) 32.9 and 37.5; 12 x 700 x 700, 40 (1.5e9) 32.6 and
+// 36.8; 16 x 1000 x 777, 40 (3.2e9) 38.9 and 48.2; 8 x 4096 x 4096, 64 (34e9) 153 and 343.  Backward: 32 x 200 x 200, 64 (0.3e9) 48 and
+// 67; 12 x 512 x 512, 32 (0.4e9) 41 and 39; 8 x 512 x 512, 40 (0.5e9) 52 and 55; 8 x 600 x 600, 96 (1.1e9) 62 and 89; the last 430 and
+// 1010.  A few rows, bound by memory, gain nothing.
 bool pair_worth(const Ctx *c, const AttnCall &a, bool grad)
 {
     const int64_t rows = (int64_t)a.n * a.group;
     if (rows == 0 || a.m == 0 || (int64_t)a.batch * a.kv_heads > 65535) return false;
     if (c->dbg_attn_pairs) return c->dbg_attn_pairs == 1;
-    return rows > 32 && 4.0 * (double)a.batch * a.kv_heads * rows * a.m * a.d * (a.causal ? 0.5 : 1.0) >= (grad ? 0.4e9 : 2.0e9);
+    return rows > 32 && 4.0 * (double)a.batch * a.kv_heads * rows * a.m * round_up(a.d, 32) * (a.causal ? 0.5 : 1.0) >= (grad ? 0.3e9 : 1.3e9);
 }
 
 size_t pair_bytes(const AttnCall &a, bool grad)
