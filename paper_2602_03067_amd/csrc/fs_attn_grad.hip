@@ -540,7 +540,7 @@ template <typename T, int DP, bool KV> void join(Ctx *c, const AttnCall &a)
     const int64_t total = (int64_t)a.batch * a.kv_heads * (KV ? 2 * (int64_t)a.m : (int64_t)a.n * a.group);
     constexpr int W = DP / 4;
     if (a.splits > 16) k_attn_grad_join<T, DP, KV, 8><<<(unsigned)ceil_div(total, 256 / (8 * W)), 256, 0, c->stream>>>(a);
-    else if (a.splits > 4) k_attn_grad_join<T, DP, KV, 4><<<(unsigned)ceil_div(total, 256 / (4 * W)), 256, 0, c->stream>>>(a);
+    else if (a.splits > 8) k_attn_grad_join<T, DP, KV, 4><<<(unsigned)ceil_div(total, 256 / (4 * W)), 256, 0, c->stream>>>(a);
     else k_attn_grad_join<T, DP, KV, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
 }
 
@@ -625,15 +625,23 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32)
 {
     AttnGradPlan p;
     const int64_t rows = (int64_t)a.n * a.group, heads = (int64_t)a.batch * a.kv_heads, dp = round_up(a.d, 32);
-    const int64_t want = 2 * (int64_t)c->num_cu;
     const int64_t qb = ceil_div(rows, 128) * heads, kb = ceil_div(a.m, 128) * heads;
     p.pairs = f32 && pair_worth(c, a, true);
     const int tile = !f32 || (p.pairs && dp <= 64) ? 64 : 32;
     const int64_t kt = ceil_div(a.m, tile), rt = ceil_div(rows, tile);
-    p.q_splits = (int)std::max<int64_t>(1, std::min(want / std::max<int64_t>(qb, 1), kt / 4));
+    // Workgroups that fill the chip (two of them in a CU's registers, or one), in splits of at least four tiles, in float32, where a tile
+    // takes longer beside the merge, two.  Backward with two, three and four, us (heads x rows x keys, d): bf16 4 x 1024 x 1024, 64: 37.2,
+    // 36.1, 34.0; 8 x 600 x 900, 128: 55, 48, 52; 8 x 512 x 512 causal, 64: 29.3, 30.0, 31.5; float32 16 x 200 x 200, 64: 39, 45, 51;
+    // 8 x 512 x 512, 64: 46, 49, 53; 12 x 1000 x 777, 40: 73, 74, 76.
+    const int64_t want = (int64_t)c->num_cu * (f32 && dp > 64 ? 1 : 2), least = f32 ? 2 : 4;
+    auto splits = [&](int64_t blocks, int64_t tiles, int64_t most) {
+        const int64_t per = std::max<int64_t>(least, ceil_div(tiles, std::max<int64_t>(1, most / std::max<int64_t>(blocks, 1))));
+        return (int)std::max<int64_t>(1, ceil_div(tiles, per));
+    };
+    p.q_splits = splits(qb, kt, want);
     // (blocks that do not fill the chip and are of unequal length, under a causal line, are cut twice as fine: short ones then fill up
     // behind long ones; 8192 points, 16 heads over 4, d = 128: 1008 us, and 1301 otherwise; where they do fill it splits cost 15 us)
-    p.k_splits = (int)std::max<int64_t>(1, kb >= want ? 1 : std::min((a.causal ? 2 : 1) * want / std::max<int64_t>(kb, 1), rt / 4));
+    p.k_splits = kb >= want ? 1 : splits(kb, rt, (a.causal ? 2 : 1) * want);
     p.q_grid = qb * p.q_splits;
     p.k_grid = kb * p.k_splits;
     p.stat_bytes = (size_t)(heads * round_up(rows, kRowBlock)) * 12;

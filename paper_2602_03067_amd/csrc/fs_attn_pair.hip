@@ -169,9 +169,10 @@ int64_t image_bytes(const AttnCall &a, int tensor)
 // The two passes and the pieces' way through memory take 8 to 15 us.  What they save grows with the products, which are padded to 32
 // coordinates.  Pairs and fp32 matrix cores, us (heads x rows x keys, d, padded operations forward), forward: 16 x 500 x 500, 64 (1.0e9)
 // 27.0 and 23.0; 8 x 600 x 600, 96 (1.1e9) 29.4 and 30.1; 4 x 800 x 800, 128 (1.3e9) 32.9 and 37.5; 12 x 700 x 700, 40 (1.5e9) 32.6 and
-// 36.8; 16 x 1000 x 777, 40 (3.2e9) 38.9 and 48.2; 8 x 4096 x 4096, 64 (34e9) 153 and 343.  Backward: 32 x 200 x 200, 64 (0.3e9) 48 and
-// 67; 12 x 512 x 512, 32 (0.4e9) 41 and 39; 8 x 512 x 512, 40 (0.5e9) 52 and 55; 8 x 600 x 600, 96 (1.1e9) 62 and 89; the last 430 and
-// 1010.  A few rows, bound by memory, gain nothing.
+// 36.8; 16 x 1000 x 777, 40 (3.2e9) 38.9 and 48.2; 8 x 4096 x 4096, 64 (34e9) 153 and 343.  Backward: 16 x 200 x 200, 64 (0.16e9) 43
+// and 39; 32 x 200 x 200, 64 (0.33e9) 48 and 45; 8 x 300 x 300, 128 (0.37e9) 57 and 66; 12 x 512 x 512, 32 (0.4e9) 37 and 43;
+// 8 x 512 x 512, 40 (0.5e9) 46 and 49; 16 x 500 x 500, 64 (1.0e9) 52 and 67; 8 x 4096 x 4096, 64 430 and 1010.  A few rows, bound by
+// memory, gain nothing.
 bool pair_worth(const Ctx *c, const AttnCall &a, bool grad)
 {
     const int64_t rows = (int64_t)a.n * a.group;
