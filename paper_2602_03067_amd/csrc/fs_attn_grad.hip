@@ -67,6 +67,13 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     const int hi = last_q < blk * 32 * WAVES / c.group ? 0 : c.causal ? min(k_len, max(0, last_q + k_len - q_len + 1)) : k_len;
     const int tiles = (hi + KT - 1) / KT, per = (tiles + c.splits - 1) / c.splits;
     const int t0 = min(tiles, split * per), t1 = min(tiles, t0 + per);
+    // D = <do, o> has o's rounding to bf16 in it, which beside the gradients of a few keys is as large as a rounding of their own.  Rows of
+    // at most 128 keys take D from its definition, sum_j p_ij <do_i, v_j>, in a sweep ahead (of all of a row's keys, in every split);
+    // further keys shrink o, and with it the error, beside the v_j.
+    constexpr bool kExact = std::is_same<T, __bf16>::value;
+    const bool few = tiles * KT <= 128;
+    int first = kExact && few ? 0 : t0;
+    const int last = kExact && few ? tiles : t1;
 
     const E *kp = (const E *)c.k + b * c.sk.batch + hk * c.sk.head;
     const E *vp = (const E *)c.v + b * c.sv.batch + hk * c.sv.head;
@@ -87,7 +94,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
             ko[i] = (unsigned)(D::row(tid, i) * (int)c.sk.row * (int)sizeof(E) + D::piece(tid, i) * 16);
             vo[i] = (unsigned)(D::row(tid, i) * (int)c.sv.row * (int)sizeof(E) + D::piece(tid, i) * 16);
         }
-        if (t0 < t1) D::clear(lds, tid, c.d, k_len - (t1 - 1) * KT, t1 - t0);
+        if (first < last) D::clear(lds, tid, c.d, k_len - (last - 1) * KT, last - first);
     }
     auto fetch = [&](int tile, int buf) {
         if constexpr (kPair) {
@@ -123,7 +130,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
         if (BIAS && tid < KT) lbias[buf][tid] = br;
     };
 
-    if (t0 < t1) fetch(t0, 0);
+    if (first < last) fetch(first, 0);
     Frag q[NS], g[NS];
     const int head = hk * c.group + pk.g;
     float delta = 0.0f;
@@ -160,6 +167,78 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
         const float2 v = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
         st = row_stat<kDiff>(v.x, v.y);
     }
+    const float unit = kDiff ? kLog2eF : scale * kLog2eF;
+    const typename TL::Lanes ln = TL::lanes(lane);
+
+    constexpr bool kRemoved = BIAS && !kPair && LOAD == kDma;
+    auto removed = [&](int buf) {
+        if constexpr (kRemoved) clear_removed<T, DP, KT, NT>(lds + 2 * buf * kTile, lds + (2 * buf + 1) * kTile, lbias[buf], tid);
+    };
+    // what a row's keys of half a tile add to its gradient
+    auto terms = [&](int tile, int buf, int nb, bool masked, f32x16 &s) {
+        const LdsPtr lk = base + 2 * buf * kTile, lv = lk + kTile;
+        f32x16 dp = (f32x16)(0.0f);
+        s = (f32x16)(0.0f);
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+            s = M::mma(TL::rows(lk, ln, nb * 32, t), q[t], s);
+            dp = M::mma(TL::rows(lv, ln, nb * 32, t), g[t], dp);
+        }
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * u + 4 * half];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], scale, add[j]);
+            }
+        }
+        if (masked) {
+            const int base = tile * KT + nb * 32 + 4 * half;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = base + 8 * (i / 4) + i % 4 < limit ? s[i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            // (without bias m is taken off in the same fma that scales)
+            const float d = BIAS ? s[i] - st.m : kDiff ? fmaf(s[i], scale, -st.m) : s[i];
+            const float p = __builtin_amdgcn_exp2f(fmaf(d, unit, -st.off));
+            s[i] = p * (kPair ? fmaf(dp[i], ps.dov, -delta) : dp[i] - delta);
+        }
+    };
+    auto begin = [&](int to) {
+        if (first < to) put(0);
+        dma_wait();
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+        if (kRemoved && first < to) removed(0);
+    };
+    auto next = [&](int tile, int buf, int to) {
+        if ((!kDirect || BIAS) && tile + 1 < to) put(buf ^ 1);
+        if (kDirect) dma_wait();
+        __syncthreads();
+        if (kRemoved && tile + 1 < to) removed(buf ^ 1);
+    };
+    begin(last);
+    if (kExact && few) {
+        float sum = 0.0f;
+        delta = 0.0f;
+        for (int tile = first; tile < last; ++tile) {
+            const int buf = (tile - first) & 1;
+            if (tile + 1 < last) fetch(tile + 1, buf ^ 1);
+            const bool masked = __any(limit < (tile + 1) * KT);
+            for (int nb = 0; nb < NB; ++nb) {
+                f32x16 s;
+                terms(tile, buf, nb, masked, s);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += s[i];
+            }
+            next(tile, buf, last);
+        }
+        delta = across_halves_sum(sum);
+        first = t0;
+        if (t0 < t1) fetch(t0, 0);
+        begin(t1);
+    }
     if (split == 0 && half == 0) {   // for the other pass, whole blocks of rows
         const int64_t pad = (int64_t)blocks * 32 * WAVES;
         float *out = c.row_stat + 3 * bh * pad + r;
@@ -167,54 +246,18 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
         out[pad] = kPair ? delta / kPairN : delta;
         if (kDiff) out[2 * pad] = st.m;
     }
-    const float unit = kDiff ? kLog2eF : scale * kLog2eF;
-    const typename TL::Lanes ln = TL::lanes(lane);
-
     f32x16 dq[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) dq[i] = (f32x16)(0.0f);
-    constexpr bool kRemoved = BIAS && !kPair && LOAD == kDma;
-    auto removed = [&](int buf) {
-        if constexpr (kRemoved) clear_removed<T, DP, KT, NT>(lds + 2 * buf * kTile, lds + (2 * buf + 1) * kTile, lbias[buf], tid);
-    };
-    if (t0 < t1) put(0);
-    dma_wait();
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    __syncthreads();
-    if (kRemoved && t0 < t1) removed(0);
     for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
-        const LdsPtr lk = base + 2 * buf * kTile, lv = lk + kTile;
+        const LdsPtr lk = base + 2 * buf * kTile;
         if (tile + 1 < t1) fetch(tile + 1, buf ^ 1);
         const bool masked = __any(limit < (tile + 1) * KT);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            f32x16 s = (f32x16)(0.0f), dp = (f32x16)(0.0f);
-#pragma unroll
-            for (int t = 0; t < NS; ++t) {
-                s = M::mma(TL::rows(lk, ln, nb * 32, t), q[t], s);
-                dp = M::mma(TL::rows(lv, ln, nb * 32, t), g[t], dp);
-            }
-            if constexpr (BIAS) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const f32x4 add = *(const f32x4 *)&lbias[buf][nb * 32 + 8 * u + 4 * half];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[4 * u + j] = fmaf(s[4 * u + j], scale, add[j]);
-                }
-            }
-            if (masked) {
-                const int base = tile * KT + nb * 32 + 4 * half;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = base + 8 * (i / 4) + i % 4 < limit ? s[i] : -INFINITY;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                // (without bias m is taken off in the same fma that scales)
-                const float d = BIAS ? s[i] - st.m : kDiff ? fmaf(s[i], scale, -st.m) : s[i];
-                const float p = __builtin_amdgcn_exp2f(fmaf(d, unit, -st.off));
-                s[i] = p * (kPair ? fmaf(dp[i], ps.dov, -delta) : dp[i] - delta);
-            }
+            f32x16 s;
+            terms(tile, buf, nb, masked, s);
 #pragma unroll
             for (int t = 0; t < NF; ++t) {
                 const Frag ds = M::pack(s, t);
@@ -222,10 +265,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
                 for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, ln, nb * 32, t, i, lane), ds, dq[i]);
             }
         }
-        if ((!kDirect || BIAS) && tile + 1 < t1) put(buf ^ 1);
-        if (kDirect) dma_wait();
-        __syncthreads();
-        if (kRemoved && tile + 1 < t1) removed(buf ^ 1);
+        next(tile, buf, t1);
     }
     if (r >= rows) return;
     if constexpr (kPair) {
