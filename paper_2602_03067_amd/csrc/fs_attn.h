@@ -81,6 +81,14 @@ template <> struct Mma<__bf16> {
         for (int j = 0; j < 8; ++j) f[j] = (__bf16)v[8 * t + j];
         return f;
     }
+    // what pack() rounds off
+    static __device__ inline Frag rest(const f32x16 &v, int t)
+    {
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (__bf16)(v[8 * t + j] - (float)(__bf16)v[8 * t + j]);
+        return f;
+    }
 };
 
 template <> struct Mma<float> {

@@ -36,7 +36,7 @@ template <typename T> constexpr int dkv_waves(int dp)
     return std::is_same<T, __bf16>::value || dp < (std::is_same<T, Pair>::value ? 96 : 64) ? 2 : 1;
 }
 
-template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD>
+template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD, bool FINE>
 __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const AttnCall c)
 {
     using M = Mma<T>;
@@ -263,6 +263,11 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
                 const Frag ds = M::pack(s, t);
 #pragma unroll
                 for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, ln, nb * 32, t, i, lane), ds, dq[i]);
+                if constexpr (FINE) {
+                    const Frag rest = M::rest(s, t);
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) dq[i] = M::mma(TL::cols(lk, ln, nb * 32, t, i, lane), rest, dq[i]);
+                }
             }
         }
         next(tile, buf, t1);
@@ -286,8 +291,8 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     for (int i = 0; i < ND; ++i) store_column<E, ALN>(out, dq[i], c.scale, 32 * i + 4 * half, c.d);
 }
 
-template <typename T, int DP, int RT, int WAVES, bool BIAS, Load LOAD>
-__global__ __launch_bounds__(64 * WAVES, dkv_waves<T>(DP)) void k_attn_dkv(const AttnCall c)
+template <typename T, int DP, int RT, int WAVES, bool BIAS, Load LOAD, bool FINE>
+__global__ __launch_bounds__(64 * WAVES, FINE && DP > 96 ? 1 : dkv_waves<T>(DP)) void k_attn_dkv(const AttnCall c)
 {
     using M = Mma<T>;
     using E = typename M::Elem;
@@ -463,6 +468,11 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves<T>(DP)) void k_attn_dkv(const
                 const Frag pf = M::pack(s, t);
 #pragma unroll
                 for (int i = 0; i < ND; ++i) dv[i] = M::mma(TL::cols(lg, ln, nb * 32, t, i, lane), pf, dv[i]);
+                if constexpr (FINE) {
+                    const Frag rest = M::rest(s, t);
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) dv[i] = M::mma(TL::cols(lg, ln, nb * 32, t, i, lane), rest, dv[i]);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -483,6 +493,11 @@ __global__ __launch_bounds__(64 * WAVES, dkv_waves<T>(DP)) void k_attn_dkv(const
                 const Frag sf = M::pack(s, t);
 #pragma unroll
                 for (int i = 0; i < ND; ++i) dk[i] = M::mma(TL::cols(lq, ln, nb * 32, t, i, lane), sf, dk[i]);
+                if constexpr (FINE) {
+                    const Frag rest = M::rest(s, t);
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) dk[i] = M::mma(TL::cols(lq, ln, nb * 32, t, i, lane), rest, dk[i]);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -604,12 +619,45 @@ template <typename T> __global__ __launch_bounds__(256) void k_attn_dbias(const 
     }
 }
 
+template <typename T, int DP, bool FINE> void dq_pass(Ctx *c, const AttnCall &a, unsigned grid, Load load)
+{
+    constexpr int N = row_tile<T>(DP);
+    constexpr Load kBest = std::is_same<T, Pair>::value ? kVec : kDma;   // (of pairs only their images are direct)
+    if (a.bias) {
+        if (load == kDma) k_attn_dq<T, DP, N, 4, true, kBest, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn_dq<T, DP, N, 4, true, kVec, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else k_attn_dq<T, DP, N, 4, true, kAny, FINE><<<grid, 256, 0, c->stream>>>(a);
+    } else {
+        if (load == kDma) k_attn_dq<T, DP, N, 4, false, kBest, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn_dq<T, DP, N, 4, false, kVec, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else k_attn_dq<T, DP, N, 4, false, kAny, FINE><<<grid, 256, 0, c->stream>>>(a);
+    }
+}
+template <typename T, int DP, bool FINE> void dkv_pass(Ctx *c, const AttnCall &a, unsigned grid, Load load)
+{
+    // (32 rows are one tile, where that is a whole number of the threads' loads)
+    constexpr int N = FINE && DP % 64 == 0 ? 32 : row_tile<T>(DP);
+    constexpr Load kBest = std::is_same<T, Pair>::value ? kVec : kDma;   // (of pairs only their images are direct)
+    if (a.bias) {
+        if (load == kDma) k_attn_dkv<T, DP, N, 4, true, kBest, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn_dkv<T, DP, N, 4, true, kVec, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else k_attn_dkv<T, DP, N, 4, true, kAny, FINE><<<grid, 256, 0, c->stream>>>(a);
+    } else {
+        if (load == kDma) k_attn_dkv<T, DP, N, 4, false, kBest, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else if (load == kVec) k_attn_dkv<T, DP, N, 4, false, kVec, FINE><<<grid, 256, 0, c->stream>>>(a);
+        else k_attn_dkv<T, DP, N, 4, false, kAny, FINE><<<grid, 256, 0, c->stream>>>(a);
+    }
+}
+
 template <typename T, int DP>
 fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Load rows_load)
 {
     using E = typename Mma<T>::Elem;
-    constexpr Load kBest = std::is_same<T, Pair>::value ? kVec : kDma;   // (of pairs only their images are direct)
-    constexpr int RT = row_tile<T>(DP), KT = RT;
+    // A few rows for each head of keys: the roundings of p and ds do not average out, and the chip is idle.  Both go on as two bf16.  (One
+    // row, 153 keys, 16 heads over 4, d = 32: dk 1.7e-3 off 64 bits, which is its own rounding, and 2.8e-3 otherwise,
+    // 19 us both; 32 rows, 2000 keys, four sets, 8 heads of 128: 44 and 39 us.)
+    constexpr bool kBf16 = std::is_same<T, __bf16>::value;
+    const bool fine = kBf16 && (int64_t)a.n * a.group <= 32;
     Arena A;
     a.row_stat = (float *)(ws + A.take(p.stat_bytes));
     float *dq_part = (float *)(ws + A.take(p.dq_bytes)), *dkv_part = (float *)(ws + A.take(p.dkv_bytes));
@@ -617,31 +665,15 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
     a.splits = p.q_splits;
     a.part = dq_part;
     if (p.q_grid) {
-        const unsigned grid = (unsigned)p.q_grid;
-        if (a.bias) {
-            if (keys == kDma) k_attn_dq<T, DP, KT, 4, true, kBest><<<grid, 256, 0, c->stream>>>(a);
-            else if (keys == kVec) k_attn_dq<T, DP, KT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dq<T, DP, KT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
-        } else {
-            if (keys == kDma) k_attn_dq<T, DP, KT, 4, false, kBest><<<grid, 256, 0, c->stream>>>(a);
-            else if (keys == kVec) k_attn_dq<T, DP, KT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dq<T, DP, KT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
-        }
+        if (fine) dq_pass<T, DP, kBf16>(c, a, (unsigned)p.q_grid, keys);
+        else dq_pass<T, DP, false>(c, a, (unsigned)p.q_grid, keys);
         if (a.splits > 1) join<E, DP, false>(c, a);
     }
     a.splits = p.k_splits;
     a.part = dkv_part;
     if (p.k_grid) {
-        const unsigned grid = (unsigned)p.k_grid;
-        if (a.bias) {
-            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, true, kBest><<<grid, 256, 0, c->stream>>>(a);
-            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, true, kVec><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dkv<T, DP, RT, 4, true, kAny><<<grid, 256, 0, c->stream>>>(a);
-        } else {
-            if (rows_load == kDma) k_attn_dkv<T, DP, RT, 4, false, kBest><<<grid, 256, 0, c->stream>>>(a);
-            else if (rows_load == kVec) k_attn_dkv<T, DP, RT, 4, false, kVec><<<grid, 256, 0, c->stream>>>(a);
-            else k_attn_dkv<T, DP, RT, 4, false, kAny><<<grid, 256, 0, c->stream>>>(a);
-        }
+        if (fine) dkv_pass<T, DP, kBf16>(c, a, (unsigned)p.k_grid, rows_load);
+        else dkv_pass<T, DP, false>(c, a, (unsigned)p.k_grid, rows_load);
         if (a.splits > 1) join<E, DP, true>(c, a);
         if (a.dbias) k_attn_dbias<E><<<dim3((unsigned)ceil_div(a.m, 16), (unsigned)a.batch), 256, 0, c->stream>>>(a);
     }
