@@ -5,4 +5,4 @@ C ABI, see ``include/flashsink.h``); ``paper_2602_03067_amd.binding`` is the thi
 ctypes layer with the same entry-point names.  Importing this package does not
 load the library; ``binding`` does, and fails loudly if it is missing.
 """
-__all__ = ["binding", "workloads", "build"]
+__all__ = ["binding", "workloads", "build", "set_encoder"]

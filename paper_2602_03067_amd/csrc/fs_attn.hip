@@ -24,6 +24,11 @@ constexpr int few_keys(int dp) { return dp > 64 ? 128 : 256; }
 // waves per SIMD: what registers allow without spills
 template <typename T> constexpr int min_waves(int dp) { return std::is_same<T, float>::value && dp >= 96 ? 1 : 2; }
 
+// Bound by the vector ALU at d = 64 (two operations and an exp2 a score beside 2 d products: 16384 points, 16 heads, bf16: 1.22 ms, 900
+// TFLOP/s, vector ALU busy 75 %, matrix cores 46 %), by the matrix cores towards d = 128 (1000 TFLOP/s), by memory for one query (50021
+// keys, 4 sets, 8 heads of 128: 113 us, 5.9 TB/s).  S^T rather than S, since its registers are a row's probabilities in the order the next
+// product takes them: they never pass through LDS.  32 rows a wave: two blocks of them a wave were slower (d = 64: 837 TFLOP/s and 843,
+// d = 128: 782 and 992), for their registers.
 // A workgroup has RW KS waves: wave w holds the w % RW-th 32 rows of the workgroup, and takes the w / RW-th part of every tile of KTS
 // keys.  With KS > 1 the parts of a row meet in LDS at the end.
 template <typename T, int DP, int KTS, int RW, int KS, bool BIAS, Load LOAD>
@@ -298,7 +303,8 @@ __global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const A
     }
 }
 
-// Merge of the splits.  A thread takes four coordinates of a packed row and every G-th split, four splits' loads at a time; G groups of
+// Merge of the splits, o = sum_s e^(m_s - m) o_s / sum_s e^(m_s - m) l_s; bound by latency (12000 rows of 40 in five splits: 5.6 us; four
+// rows of 128 a head in 32 splits: 4.9 us).  A thread takes four coordinates of a packed row and every G-th split, four splits' loads at a time; G groups of
 // threads share a row and meet in LDS: one up to eight splits (five splits of 12000 rows, d = 40 in float32: 40.3 us with the splits'
 // own kernel; four groups, whose loads mostly repeat a split: 43.0).
 template <typename T, int DP, int G>

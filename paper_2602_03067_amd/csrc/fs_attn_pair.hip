@@ -56,7 +56,9 @@ template <int N> __device__ inline void load_row(const float *row, int col, int 
     }
 }
 
-// eight lanes take a row, each DP / 8 elements of it; a workgroup 32 rows at a time
+// Bound by latency at the sizes that gain from pairs (three sets of 1000 and 777 points, 4 heads of 40, four tensors: 5.7 us, and 7.3 for
+// the second pass, of which some 2 are each launch's own).
+// Eight lanes take a row, each DP / 8 elements of it; a workgroup 32 rows at a time
 template <int DP> __global__ __launch_bounds__(256) void k_pair_max(const AttnCall c, bool aligned)
 {
     __shared__ float2 lds[4];
@@ -101,7 +103,7 @@ __device__ inline float scale_of(float top)
     return __builtin_bit_cast(float, (uint32_t)e << 23);
 }
 
-// a workgroup writes 32 rows
+// A workgroup writes 32 rows as the attention kernels' LDS holds them, so that these fetch tiles with direct loads of whole lines.
 template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const AttnCall c, bool aligned)
 {
     using TL = Tile<Pair, DP>;
