@@ -24,6 +24,9 @@ constexpr int few_keys(int dp) { return dp > 64 ? 128 : 256; }
 // waves per SIMD: what registers allow without spills
 template <typename T> constexpr int min_waves(int dp) { return std::is_same<T, float>::value && dp >= 96 ? 1 : 2; }
 
+// What a row reports as its largest score: NaN where a score is NaN, which fmaxf leaves out (of infinite scores the sum alone is NaN).
+__device__ inline float reported_max(float top, float sum) { return sum != sum && top < INFINITY ? sum : top; }
+
 // Bound by the vector ALU at d = 64 (two operations and an exp2 a score beside 2 d products: 16384 points, 16 heads, bf16: 1.22 ms, 900
 // TFLOP/s, vector ALU busy 75 %, matrix cores 46 %), by the matrix cores towards d = 128 (1000 TFLOP/s), by memory for one query (50021
 // keys, 4 sets, 8 heads of 128: 113 us, 5.9 TB/s).  S^T rather than S, since its registers are a row's probabilities in the order the next
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(64 * RW * KS, min_waves<T>(DP)) void k_attn(const A
         const int64_t at = (bh * c.group + pk.g) * c.n + pk.q;
         // the sum below the maximum itself
         const float safe = ref == -INFINITY ? 0.0f : ref;
-        *(float2 *)(c.stat + 2 * at) = make_float2(top * st, sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f((safe - top) * unit));
+        *(float2 *)(c.stat + 2 * at) = make_float2(reported_max(top * st, sum), sum == 0.0f ? 0.0f : sum * __builtin_amdgcn_exp2f((safe - top) * unit));
     }
 }
 
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnCall c)
     float top = -INFINITY, sum = 0.0f;   // the largest score of all, and the sum below it
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     auto add = [&](float mx, float ref, float s, f32x4 v) {   // the split's largest score, what it was taken below, its sums
-        if (ref == -INFINITY) return;   // no key of this split
+        if (ref == -INFINITY && s == s) return;   // no key of this split (with scores that are all NaN the sum is NaN as well)
         const float next = fmaxf(top, mx), f = __builtin_amdgcn_exp2f((top - next) * kLog2eF), h = __builtin_amdgcn_exp2f((ref - next) * kLog2eF);
         top = next;
         sum = fmaf(sum, f, s * h);
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnCall c)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (4 * x + j < c.d) out[4 * x + j] = (T)(acc[j] * inv);
-    if (x == 0) *(float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q)) = make_float2(top, sum);
+    if (x == 0) *(float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q)) = make_float2(reported_max(top, sum), sum);
 }
 
 template <typename T, int DP> void join(Ctx *c, const AttnCall &a)
