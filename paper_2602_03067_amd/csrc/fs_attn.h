@@ -452,7 +452,8 @@ __device__ inline PairScale pair_scale(const AttnCall &c, int64_t bh)
     const float *s = c.pair.scale + 8 * bh;
     const float q = 1.0f / s[kPairQ], k = 1.0f / s[kPairK], v = 1.0f / s[kPairV];
     PairScale p;
-    p.score = c.scale * q * k;
+    // (in 64 bits, and inside the normal floats: what is removed is minus infinity times this, also where all scores are as good as zero)
+    p.score = (float)fmin(fmax((double)c.scale * q * k, 0x1p-126), 0x1p126);
     p.v = v;
     p.dov = p.ds = p.dq = p.dk = p.dv = 0.0f;
     if (c.pair.img[kPairDo]) {
