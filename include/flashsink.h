@@ -397,9 +397,13 @@ fs_status fs_points_release(fs_ctx *ctx);
  * kv_heads divides q_heads; head h reads keys and values of head h / (q_heads / kv_heads).  d <= 128 coordinates.
  * Lengths may be 0 and 1, strides are in elements, any alignment will do (rows of whole 16 bytes, aligned to them, are
  * read fastest).
- * FS_F32: products on the fp32 matrix cores; where that takes long enough (2e9 operations forward),
- * from operands in two fp16 pieces, 22 bits of every element down to 2^-17 of its head's largest and 2^-40 of that below, summed in
- * fp32.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
+ * FS_F32: products on the fp32 matrix cores, or, where that takes long enough (4 batch q_heads q_rows k_rows d operations, d rounded up to
+ * 32, half of them under a causal line: 1.3e9 forward, 0.3e9 backward, and more than 32 rows a head of keys), from operands in two
+ * fp16 pieces, summed in fp32.  They hold 22 bits of every element of q, k and v down to 2^-17 of its head's largest, of the gradient
+ * d_o down to 2^-17 of its row's largest, and what is smaller to 2^-39 of that largest.  For dq gradients of scores keep 22 bits of what
+ * is largest in their row.  dk, dv and dbias are sums over rows: there gradients of scores are kept to 2^-38 of the head's largest
+ * |d_o_i| |v| / l_i, probabilities to 2^-40 of one, so keys that only rows of far smaller d_o see, or that no row gives a probability to
+ * speak of, have gradients of fewer digits.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
  * probabilities (2^-9 of each) and their gradients are rounded to bf16 where they enter a second product.  Maxima, sums
  * and accumulators are fp32 in both.
  */

@@ -24,8 +24,8 @@ template <typename T> struct Mma;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// Floats as the sum of two fp16, under a power of two for all of a head's rows that puts the largest into [2^14, 2^15): 22 bits of
-// every element down to 2^-17 of the largest, and never less than 2^-40 of it.  A product takes three products of the pieces
+// Floats as the sum of two fp16, under a power of two for all of a head's rows (of do: for each) that puts the largest into [2^14, 2^15):
+// 22 bits of every element down to 2^-17 of the largest, and never less than 2^-40 of it.  A product takes three products of the pieces
 // (the two lower ones' is below 2^-22), three v_mfma_f32_32x32x16_f16 of 32 cycles for sixteen coordinates, where the fp32
 // matrix cores take eight of 64.
 struct Pair {};
@@ -325,15 +325,17 @@ struct HeadsAt {
 };
 
 // Pairs of a call in the workspace: per (set, kv head) tiles of 32 packed rows (or keys), padded to 128 rows, zero where nothing is
-// admitted; and eight floats: the scales of q, k, v and do (powers of two) and the largest row norms of v and do.
+// admitted; and eight floats: the scales of q, k and v and the smallest of the rows of do (powers of two), the largest row norm of v, and
+// that of do over the row's sum of exponentials.
 enum { kPairQ, kPairK, kPairV, kPairDo, kPairTensors };
 struct PairImage {
     char *img[kPairTensors];
     float *scale;
+    f32x4 *row;    // of the rows of do, padded like them: the scale; <do, o> of do times 2^-15 of it; |do| times it; 0
     float *part;   // maxima of chunks of rows
 };
 constexpr float kPairP = 16.0f;      // probabilities below a reference enter the second product times this (up to 2^11: attn_slack)
-constexpr float kPairN = 32768.0f;   // normalised ones times this
+constexpr float kPairN = 32768.0f;   // normalised ones times this (2^15)
 
 __host__ __device__ inline int64_t pair_rows(int64_t rows) { return (rows + 127) / 128 * 128; }
 
@@ -439,35 +441,64 @@ AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32);
 // `ws`: the bytes of the plan, each piece rounded up to 256
 fs_status launch_attn_grad(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, bool f32, bool aligned);
 
-// What turns products of pieces into what they stand for (all powers of two but the first).  The gradient of a score is at most 2 |do| |v|
-// in size: times `ds`, from the largest norms, it is inside fp16.
+// the power of two that puts `top` into [2^e, 2^(e + 1)), as far as floats go; 1 where there is nothing to scale
+__device__ inline float pair_power(float top, int e)
+{
+    if (!(top > 0.0f && top < INFINITY)) return 1.0f;
+    e += 254 - (int)(__builtin_bit_cast(uint32_t, top) >> 23);
+    e = e < 1 ? 1 : e > 240 ? 240 : e;
+    return __builtin_bit_cast(float, (uint32_t)e << 23);
+}
+__device__ inline int pair_exponent(float v) { return (int)(__builtin_bit_cast(uint32_t, v) >> 23) - 127; }
+__device__ inline float pair_mantissa(float v) { return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, v) & 0x7fffffu) | 0x3f800000u); }
+__device__ inline float pair_two(int e) { return __builtin_bit_cast(float, (uint32_t)((e < -126 ? -126 : e > 127 ? 127 : e) + 127) << 23); }   // 2^e
+
+// What turns products of pieces into what they stand for.
 struct PairScale {
     float score;   // of <q, k>, with the call's own scale
-    float v, dov;  // 1 / scale of v, ds / (scales of do and v)
-    float ds;
-    float dq, dk, dv;   // of the sums over ds k, ds q and kPairN p do
+    float v;       // 1 / scale of v
 };
 __device__ inline PairScale pair_scale(const AttnCall &c, int64_t bh)
 {
     const float *s = c.pair.scale + 8 * bh;
-    const float q = 1.0f / s[kPairQ], k = 1.0f / s[kPairK], v = 1.0f / s[kPairV];
+    const float q = 1.0f / s[kPairQ], k = 1.0f / s[kPairK];
     PairScale p;
     // (in 64 bits, and inside the normal floats: what is removed is minus infinity times this, also where all scores are as good as zero)
     p.score = (float)fmin(fmax((double)c.scale * q * k, 0x1p-126), 0x1p126);
-    p.v = v;
-    p.dov = p.ds = p.dq = p.dk = p.dv = 0.0f;
-    if (c.pair.img[kPairDo]) {
-        const float g = 1.0f / s[kPairDo], n = s[4] * s[5];
-        int e = 127 + 13 - ((int)(__builtin_bit_cast(uint32_t, n) >> 23) - 127);   // n < 2^(e + 1): ds n in (2^12, 2^14]
-        e = e < 1 ? 1 : e > 240 ? 240 : e;
-        p.ds = n == 0.0f ? 1.0f : __builtin_bit_cast(float, (uint32_t)e << 23);
-        p.dov = p.ds * g * v;
-        p.dq = k / p.ds;
-        p.dk = q / p.ds;
-        p.dv = g / kPairN;
-    }
+    p.v = 1.0f / s[kPairV];
     return p;
 }
+// ... and of the backward pass.  The gradient of a score, p_ij (<do_i, v_j> - D_i), is at most 2 |do_i| |v| / l_i in size: l_i is the sum
+// of exponentials that the largest is one of.  It enters the product for dq, a row's own, under a power of two of that row, from its |do_i|
+// and l_i, so that it has its 22 bits in every row.  dk and dv are sums over rows: there it is under one for the head, `ds`, from the
+// largest |do_i| / l_i, and p_ij under kPairN times the share of the row's do in the head's largest (do has a scale for every row).
+struct PairGrad {
+    float top;       // the largest |v| in units of its pieces
+    float scale_v;
+    int v, g, ds;    // exponents: of the scales of v and of the row of do that has the smallest, and of what puts the head's largest
+                     // gradient of a score into [2^13, 2^14)
+    float dov;       // ds / (scale of v, g, kPairN): of products of pieces of do and v, and of D in their units
+};
+__device__ inline PairGrad pair_grad(const AttnCall &c, int64_t bh)
+{
+    const float *s = c.pair.scale + 8 * bh;
+    PairGrad p;
+    p.scale_v = s[kPairV];
+    p.top = s[4] * p.scale_v;
+    p.v = pair_exponent(p.scale_v);
+    p.g = pair_exponent(s[kPairDo]);
+    const float a = s[4], b = s[5];   // (their product need not be a float)
+    const int e = pair_exponent(a) + pair_exponent(b);
+    const float m = pair_mantissa(a) * pair_mantissa(b);
+    p.ds = a > 0.0f && b > 0.0f && a < INFINITY && b < INFINITY ? 13 - 1 - e - (m >= 2.0f) : 0;
+    p.dov = pair_two(p.ds - p.v - p.g - 15);
+    return p;
+}
+// f 2^e in two factors: what is of moderate size stays a float between them if it is one after both.
+struct PairFactor {
+    float a, b;
+};
+__device__ inline PairFactor pair_factor(float f, int e) { return {pair_two(e / 2), f * pair_two(e - e / 2)}; }
 
 __device__ inline float across_halves_max(float v)
 {

@@ -81,9 +81,10 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     const E *kp = (const E *)c.k + b * c.sk.batch + hk * c.sk.head;
     const E *vp = (const E *)c.v + b * c.sv.batch + hk * c.sv.head;
     const int64_t bh = (int64_t)b * c.kv_heads + hk;
-    PairScale ps;
-    if constexpr (kPair) ps = pair_scale(c, bh);
-    const float scale = kPair ? ps.score : c.scale;
+    PairGrad pg;
+    if constexpr (kPair) pg = pair_grad(c, bh);
+    float own = 1.0f;   // pairs: the power of two of the row's gradients of scores, in units of the pieces
+    const float scale = kPair ? pair_scale(c, bh).score : c.scale;
     const float *bp = BIAS ? c.bias + b * c.bias_ld : nullptr;
     const LdsPtr base = (LdsPtr)lds;
 
@@ -137,38 +138,37 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     Frag q[NS], g[NS];
     const int head = hk * c.group + pk.g;
     float delta = 0.0f;
+    f32x4 own_row;   // pairs: see PairImage
     {
-        using P = std::conditional_t<kPair, Mma<float>, M>;   // (how the tensors themselves are read)
-        const E *rq = (const E *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + head * c.sq.head;
-        const E *rg = (const E *)c.d_o + b * c.s_do.batch + (int64_t)pk.q * c.s_do.row + head * c.s_do.head;
-        const E *ro = (const E *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + head * c.so.head;
-        const uint4 z = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int t = 0; t < DP / P::kStep; ++t) {
-            const auto gt = __builtin_bit_cast(typename P::Frag, live ? load_piece<E, ALN>(rg, 2 * t + half, c.d) : z);
-            const auto ot = __builtin_bit_cast(typename P::Frag, live ? load_piece<E, ALN>(ro, 2 * t + half, c.d) : z);
-#pragma unroll
-            for (int j = 0; j < P::kPiece; ++j) delta = fmaf((float)gt[j], (float)ot[j], delta);
-            if constexpr (!kPair) {
-                q[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(rq, 2 * t + half, c.d) : z);
-                g[t] = gt;
-            }
-        }
         if constexpr (kPair) {
-            const int64_t at = bh * pair_rows(rows) * TL::kRow;
+            const int64_t at = bh * pair_rows(rows);
 #pragma unroll
             for (int t = 0; t < NS; ++t) {
-                q[t] = TL::from_image(c.pair.img[kPairQ] + at, r, t, half);
-                g[t] = TL::from_image(c.pair.img[kPairDo] + at, r, t, half);
+                q[t] = TL::from_image(c.pair.img[kPairQ] + at * TL::kRow, r, t, half);
+                g[t] = TL::from_image(c.pair.img[kPairDo] + at * TL::kRow, r, t, half);
+            }
+            own_row = c.pair.row[at + r];
+        } else {
+            const E *rq = (const E *)c.q + b * c.sq.batch + (int64_t)pk.q * c.sq.row + head * c.sq.head;
+            const E *rg = (const E *)c.d_o + b * c.s_do.batch + (int64_t)pk.q * c.s_do.row + head * c.s_do.head;
+            const E *ro = (const E *)c.o + b * c.so.batch + (int64_t)pk.q * c.so.row + head * c.so.head;
+            const uint4 z = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                q[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(rq, 2 * t + half, c.d) : z);
+                g[t] = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(rg, 2 * t + half, c.d) : z);
+                const auto ot = __builtin_bit_cast(Frag, live ? load_piece<E, ALN>(ro, 2 * t + half, c.d) : z);
+#pragma unroll
+                for (int j = 0; j < M::kPiece; ++j) delta = fmaf((float)g[t][j], (float)ot[j], delta);
             }
         }
     }
-    delta = across_halves_sum(delta);
-    if (kPair) delta *= ps.ds;
+    delta = kPair ? own_row[1] * pg.scale_v * 0x1p15f : across_halves_sum(delta);
     RowStat st = {0.0f, INFINITY};
     if (live) {
         const float2 v = *(const float2 *)(c.stat + 2 * ((bh * c.group + pk.g) * c.n + pk.q));
         st = row_stat<kDiff>(v.x, v.y);
+        if constexpr (kPair) own = pair_power(2.0f * own_row[2] * pg.top * __builtin_amdgcn_rcpf(v.y), 13);
     }
     const float unit = kDiff ? kLog2eF : scale * kLog2eF;
     const typename TL::Lanes ln = TL::lanes(lane);
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
             // (without bias m is taken off in the same fma that scales)
             const float d = BIAS ? s[i] - st.m : kDiff ? fmaf(s[i], scale, -st.m) : s[i];
             const float p = __builtin_amdgcn_exp2f(fmaf(d, unit, -st.off));
-            s[i] = p * (kPair ? fmaf(dp[i], ps.dov, -delta) : dp[i] - delta);
+            s[i] = p * (kPair ? fmaf(dp[i], own, -delta) : dp[i] - delta);
         }
     };
     auto begin = [&](int to) {
@@ -245,10 +245,16 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     if (split == 0 && half == 0) {   // for the other pass, whole blocks of rows
         const int64_t pad = (int64_t)blocks * 32 * WAVES;
         float *out = c.row_stat + 3 * bh * pad + r;
-        out[0] = kPair ? st.off - 15.0f : st.off;   // (probabilities times kPairN = 2^15)
-        out[pad] = kPair ? delta / kPairN : delta;
+        if constexpr (kPair) {   // (probabilities times kPairN = 2^15 and the share of the row's do)
+            out[0] = st.off + (float)(pair_exponent(own_row[0]) - pg.g - 15);
+            out[pad] = delta * pg.dov;
+        } else {
+            out[0] = st.off;
+            out[pad] = delta;
+        }
         if (kDiff) out[2 * pad] = st.m;
     }
+    if (kPair) delta *= own;
     f32x16 dq[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) dq[i] = (f32x16)(0.0f);
@@ -277,8 +283,9 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     }
     if (r >= rows) return;
     if constexpr (kPair) {
+        const PairFactor f = pair_factor(c.scale, -(pair_exponent(own) + pair_exponent(own_row[0]) + pg.v + pair_exponent(c.pair.scale[8 * bh + kPairK])));
 #pragma unroll
-        for (int i = 0; i < ND; ++i) dq[i] *= ps.dq;
+        for (int i = 0; i < ND; ++i) dq[i] = dq[i] * f.a * f.b;
     }
     if (c.splits > 1) {
         float *po = c.part + ((int64_t)split * c.batch * c.kv_heads * rows + bh * rows + r) * DP + 4 * half;
@@ -291,7 +298,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
     }
     E *out = (E *)c.dq + b * c.sdq.batch + (int64_t)pk.q * c.sdq.row + head * c.sdq.head;
 #pragma unroll
-    for (int i = 0; i < ND; ++i) store_column<E, ALN>(out, dq[i], c.scale, 32 * i + 4 * half, c.d);
+    for (int i = 0; i < ND; ++i) store_column<E, ALN>(out, dq[i], kPair ? 1.0f : c.scale, 32 * i + 4 * half, c.d);
 }
 
 // Keys in registers, rows streamed: S = Q K^T and dP = dO V^T end as a key's p and ds in the order dV^T += dO^T P and dK^T += Q^T dS take
@@ -335,9 +342,9 @@ __global__ __launch_bounds__(64 * WAVES, FINE && DP > 96 ? 1 : dkv_waves<T>(DP))
 
     const E *qp = (const E *)c.q + b * c.sq.batch + (int64_t)hk * c.group * c.sq.head;
     const E *gp = (const E *)c.d_o + b * c.s_do.batch + (int64_t)hk * c.group * c.s_do.head;
-    PairScale ps;
-    if constexpr (kPair) ps = pair_scale(c, bh);
-    const float scale = kPair ? ps.score : c.scale, dov = kPair ? ps.dov / kPairN : 1.0f;
+    PairGrad pg;
+    if constexpr (kPair) pg = pair_grad(c, bh);
+    const float scale = kPair ? pair_scale(c, bh).score : c.scale;
     const int64_t pad = round_up_rows(rows);
     const float *sp = c.row_stat + 3 * bh * pad;
     const LdsPtr base = (LdsPtr)lds;
@@ -489,7 +496,7 @@ __global__ __launch_bounds__(64 * WAVES, FINE && DP > 96 ? 1 : dkv_waves<T>(DP))
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int i = 4 * u + j;
-                    s[i] *= kPair ? fmaf(dp[i], dov, -dl[j]) : dp[i] - dl[j];
+                    s[i] *= kPair ? fmaf(dp[i], pg.dov, -dl[j]) : dp[i] - dl[j];
                     if (BIAS) db += s[i];
                 }
             }
@@ -519,12 +526,14 @@ __global__ __launch_bounds__(64 * WAVES, FINE && DP > 96 ? 1 : dkv_waves<T>(DP))
         db = 0.0f;
     }
     if constexpr (kPair) {
+        const PairFactor f = pair_factor(c.scale, -(pg.ds + pair_exponent(c.pair.scale[8 * bh + kPairQ]))), fb = pair_factor(1.0f, -pg.ds),
+                         fv = pair_factor(1.0f, -15 - pg.g);
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-            dk[i] *= ps.dk;
-            dv[i] *= ps.dv;
+            dk[i] = dk[i] * f.a * f.b;
+            dv[i] = dv[i] * fv.a * fv.b;
         }
-        db /= ps.ds;
+        db = db * fb.a * fb.b;
     }
     const int64_t slot = ((int64_t)split * c.batch * c.kv_heads + bh) * c.m + key;
     if (BIAS && c.dbias && half == 0) c.dbias_part[slot] = db;
@@ -543,14 +552,15 @@ __global__ __launch_bounds__(64 * WAVES, FINE && DP > 96 ? 1 : dkv_waves<T>(DP))
     E *ov = (E *)c.dv + b * c.sdv.batch + (int64_t)key * c.sdv.row + hk * c.sdv.head;
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-        store_column<E, ALN>(ok, dk[i], c.scale, 32 * i + 4 * half, c.d);
+        store_column<E, ALN>(ok, dk[i], kPair ? 1.0f : c.scale, 32 * i + 4 * half, c.d);
         store_column<E, ALN>(ov, dv[i], 1.0f, 32 * i + 4 * half, c.d);
     }
 }
 
-// Sums over the splits, in an order that does not depend on anything else: of dq, or (KV) of dk and dv.  A thread takes four coordinates of a
+// Sums over the splits, in an order that does not depend on anything else: of dq, or (KV) of dk and dv; dq and dk times the call's scale
+// (SCALED: they have it already).  A thread takes four coordinates of a
 // row and every G-th split, four splits' loads at a time; G groups of threads share a row and meet in LDS.
-template <typename T, int DP, bool KV, int G>
+template <typename T, int DP, bool KV, bool SCALED, int G>
 __global__ __launch_bounds__(256) void k_attn_grad_join(const AttnCall c)
 {
     constexpr int W = DP / 4, R = 256 / (W * G);
@@ -579,7 +589,7 @@ __global__ __launch_bounds__(256) void k_attn_grad_join(const AttnCall c)
     const int64_t row = KV ? at / 2 : at, bh = row / rows;
     const int hk = (int)(bh % c.kv_heads), b = (int)(bh / c.kv_heads), r = (int)(row - bh * rows);
     T *out;
-    float f = c.scale;
+    float f = SCALED ? 1.0f : c.scale;
     if constexpr (KV) {
         if (at % 2 == 0) {
             out = (T *)c.dk + b * c.sdk.batch + (int64_t)r * c.sdk.row + hk * c.sdk.head;
@@ -596,13 +606,13 @@ __global__ __launch_bounds__(256) void k_attn_grad_join(const AttnCall c)
         if (4 * x + j < c.d) out[4 * x + j] = (T)(acc[j] * f);
 }
 
-template <typename T, int DP, bool KV> void join(Ctx *c, const AttnCall &a)
+template <typename T, int DP, bool KV, bool SCALED> void join(Ctx *c, const AttnCall &a)
 {
     const int64_t total = (int64_t)a.batch * a.kv_heads * (KV ? 2 * (int64_t)a.m : (int64_t)a.n * a.group);
     constexpr int W = DP / 4;
-    if (a.splits > 16) k_attn_grad_join<T, DP, KV, 8><<<(unsigned)ceil_div(total, 256 / (8 * W)), 256, 0, c->stream>>>(a);
-    else if (a.splits > 8) k_attn_grad_join<T, DP, KV, 4><<<(unsigned)ceil_div(total, 256 / (4 * W)), 256, 0, c->stream>>>(a);
-    else k_attn_grad_join<T, DP, KV, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
+    if (a.splits > 16) k_attn_grad_join<T, DP, KV, SCALED, 8><<<(unsigned)ceil_div(total, 256 / (8 * W)), 256, 0, c->stream>>>(a);
+    else if (a.splits > 8) k_attn_grad_join<T, DP, KV, SCALED, 4><<<(unsigned)ceil_div(total, 256 / (4 * W)), 256, 0, c->stream>>>(a);
+    else k_attn_grad_join<T, DP, KV, SCALED, 1><<<(unsigned)ceil_div(total, 256 / W), 256, 0, c->stream>>>(a);
 }
 
 // Sum over the splits and heads that share a bias: sixteen lanes take a key each, sixteen shares side by side.
@@ -662,7 +672,7 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
     // A few rows for each head of keys: the roundings of p and ds do not average out, and the chip is idle.  Both go on as two bf16.  (One
     // row, 153 keys, 16 heads over 4, d = 32: dk 1.7e-3 off 64 bits, which is its own rounding, and 2.8e-3 otherwise,
     // 19 us both; 32 rows, 2000 keys, four sets, 8 heads of 128: 44 and 39 us.)
-    constexpr bool kBf16 = std::is_same<T, __bf16>::value;
+    constexpr bool kBf16 = std::is_same<T, __bf16>::value, kPairs = std::is_same<T, Pair>::value;
     const bool fine = kBf16 && (int64_t)a.n * a.group <= 32;
     Arena A;
     a.row_stat = (float *)(ws + A.take(p.stat_bytes));
@@ -673,14 +683,14 @@ fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Lo
     if (p.q_grid) {
         if (fine) dq_pass<T, DP, kBf16>(c, a, (unsigned)p.q_grid, keys);
         else dq_pass<T, DP, false>(c, a, (unsigned)p.q_grid, keys);
-        if (a.splits > 1) join<E, DP, false>(c, a);
+        if (a.splits > 1) join<E, DP, false, kPairs>(c, a);
     }
     a.splits = p.k_splits;
     a.part = dkv_part;
     if (p.k_grid) {
         if (fine) dkv_pass<T, DP, kBf16>(c, a, (unsigned)p.k_grid, rows_load);
         else dkv_pass<T, DP, false>(c, a, (unsigned)p.k_grid, rows_load);
-        if (a.splits > 1) join<E, DP, true>(c, a);
+        if (a.splits > 1) join<E, DP, true, kPairs>(c, a);
         if (a.dbias) k_attn_dbias<E><<<dim3((unsigned)ceil_div(a.m, 16), (unsigned)a.batch), 256, 0, c->stream>>>(a);
     }
     FS_HIP(c, hipGetLastError());

@@ -18,11 +18,12 @@ struct Rows {
     bool keys;
     int count;           // packed rows, or keys
 };
+constexpr int kPairO = kPairTensors;   // (not kept in pieces)
 __device__ inline Rows rows_of(const AttnCall &c, int tensor, int bh)
 {
     const int b = bh / c.kv_heads, hk = bh - b * c.kv_heads;
-    const HeadsAt at = tensor == kPairQ ? c.sq : tensor == kPairK ? c.sk : tensor == kPairV ? c.sv : c.s_do;
-    const void *p = tensor == kPairQ ? c.q : tensor == kPairK ? c.k : tensor == kPairV ? c.v : c.d_o;
+    const HeadsAt at = tensor == kPairQ ? c.sq : tensor == kPairK ? c.sk : tensor == kPairV ? c.sv : tensor == kPairO ? c.so : c.s_do;
+    const void *p = tensor == kPairQ ? c.q : tensor == kPairK ? c.k : tensor == kPairV ? c.v : tensor == kPairO ? c.o : c.d_o;
     const bool keys = tensor == kPairK || tensor == kPairV;
     return {(const float *)p + b * at.batch + (int64_t)(keys ? hk : hk * c.group) * at.head, at, keys, keys ? c.m : c.n * c.group};
 }
@@ -36,6 +37,15 @@ __device__ inline const float *row_at(const AttnCall &c, const Rows &t, int b, i
     const Packed pk = unpack(r, c.group);
     const int len = c.q_len ? min(max(c.q_len[b], 0), c.n) : c.n;
     return pk.q < len ? t.p + (int64_t)pk.q * t.at.row + pk.g * t.at.head : nullptr;
+}
+
+// what a row's norm counts: of do over the sum of exponentials, the row's largest probability (a row that sees no key: nothing)
+__device__ inline float weight_of(const AttnCall &c, int tensor, int bh, int r)
+{
+    if (tensor != kPairDo) return 1.0f;
+    const Packed pk = unpack(r, c.group);
+    const float l = c.stat[2 * (((int64_t)bh * c.group + pk.g) * c.n + pk.q) + 1];
+    return l > 0.0f ? 1.0f / l : 0.0f;
 }
 
 // `count` elements of a row from `col` on, zero beyond d (ALN: aligned to 16 bytes, d a multiple of four)
@@ -69,6 +79,7 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_max(const AttnCa
     float top = 0.0f, norm = 0.0f;
     for (int r = r0 + threadIdx.x / 8; r < r1; r += 32) {
         float v[DP / 8];
+        const float weight = weight_of(c, tensor, bh, r);
         load_row<DP / 8>(row_at(c, t, bh / c.kv_heads, r), x * (DP / 8), c.d, aligned, v);
         double s = 0.0;   // (squares leave a float's range before the values do)
 #pragma unroll
@@ -79,7 +90,7 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_max(const AttnCa
             }
 #pragma unroll
         for (int m = 1; m < 8; m *= 2) s += __shfl_xor(s, m);
-        norm = fmaxf(norm, (float)sqrt(s));
+        norm = fmaxf(norm, (float)sqrt(s) * weight);
     }
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
@@ -94,16 +105,8 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_max(const AttnCa
     }
 }
 
-// the power of two that puts `top` into [2^14, 2^15)
-__device__ inline float scale_of(float top)
-{
-    if (top == 0.0f) return 1.0f;
-    int e = 127 + 14 - ((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127);
-    e = e < 1 ? 1 : e > 240 ? 240 : e;
-    return __builtin_bit_cast(float, (uint32_t)e << 23);
-}
-
-// A workgroup writes 32 rows as the attention kernels' LDS holds them, so that these fetch tiles with direct loads of whole lines.
+// A workgroup writes 32 rows as the attention kernels' LDS holds them, so that these fetch tiles with direct loads of whole lines; of do
+// every row under its own scale, with what the backward pass needs of it besides.
 template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const AttnCall c, bool aligned)
 {
     using TL = Tile<Pair, DP>;
@@ -112,12 +115,16 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const Attn
     const Rows t = rows_of(c, tensor, bh);
     const int64_t pad = pair_rows(t.count);
     if ((int64_t)blockIdx.x * 32 >= pad) return;
-    constexpr int P = 32 * DP / 8, N = (P + 255) / 256;   // pieces of eight elements
-    float v[N][8];   // (on their way while the scale is found)
+    constexpr int W = DP / 8, P = 32 * W, N = (P + 255) / 256;   // pieces of eight elements, of a row and of all
+    __shared__ float piece_top[P];
+    __shared__ float2 piece_sum[P];
+    float v[N][8], o[N][8];   // (on their way while the scale is found)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int p = threadIdx.x + 256 * i, r = blockIdx.x * 32 + p / (DP / 8);
-        load_row<8>(p < P && r < t.count ? row_at(c, t, bh / c.kv_heads, r) : nullptr, p % (DP / 8) * 8, c.d, aligned, v[i]);
+        const int p = threadIdx.x + 256 * i, r = blockIdx.x * 32 + p / W;
+        load_row<8>(p < P && r < t.count ? row_at(c, t, bh / c.kv_heads, r) : nullptr, p % W * 8, c.d, aligned, v[i]);
+        if (tensor == kPairDo)
+            load_row<8>(p < P && r < t.count ? row_at(c, rows_of(c, kPairO, bh), bh / c.kv_heads, r) : nullptr, p % W * 8, c.d, aligned, o[i]);
     }
     float top = 0.0f, norm = 0.0f;
     for (int i = threadIdx.x; i < chunks(t.count); i += 256) {
@@ -131,32 +138,74 @@ template <int DP> __global__ __launch_bounds__(256) void k_pair_split(const Attn
         norm = fmaxf(norm, __shfl_xor(norm, m));
     }
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(top, norm);
+    if (tensor == kPairDo) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = threadIdx.x + 256 * i;
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fabsf(v[i][j]) < INFINITY ? fmaxf(m, fabsf(v[i][j])) : m;
+            if (p < P) piece_top[p] = m;
+        }
+    }
     __syncthreads();
     top = fmaxf(fmaxf(lds[0].x, lds[1].x), fmaxf(lds[2].x, lds[3].x));
     norm = fmaxf(fmaxf(lds[0].y, lds[1].y), fmaxf(lds[2].y, lds[3].y));
-    const float scale = scale_of(top);
+    const float scale = pair_power(top, 14);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         c.pair.scale[8 * bh + tensor] = scale;
         if (tensor >= kPairV) c.pair.scale[8 * bh + 4 + tensor - kPairV] = norm;
     }
+    float row_own[N];
     char *img = c.pair.img[tensor] + ((int64_t)bh * pad + (int64_t)blockIdx.x * 32) * TL::kRow;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int p = threadIdx.x + 256 * i;
         if (p >= P) break;
+        float own = scale;
+        if (tensor == kPairDo) {
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) m = fmaxf(m, piece_top[p / W * W + j]);
+            if (m > 0.0f) own = pair_power(m, 14);   // (never below the head's; a row of zeros takes that)
+            if (p % W == 0) row_own[i] = own;
+            float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = v[i][j] * (own * 0x1p-15f);
+                sum.x = fmaf(x, o[i][j], sum.x);
+                sum.y = fmaf(x, x, sum.y);
+            }
+            piece_sum[p] = sum;
+        }
         f16x8 h, l;
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             f16x2 a, b;
-            Mma<Pair>::split(v[i][j] * scale, v[i][j + 1] * scale, a, b);
+            Mma<Pair>::split(v[i][j] * own, v[i][j + 1] * own, a, b);
             h[j] = a[0];
             h[j + 1] = a[1];
             l[j] = b[0];
             l[j + 1] = b[1];
         }
-        const int at = TL::B::at(p / (DP / 8), p % (DP / 8));
+        const int at = TL::B::at(p / W, p % W);
         *(f16x8 *)(img + at) = h;
         *(f16x8 *)(img + TL::kLower + at) = l;
+    }
+    if (tensor != kPairDo) return;
+    // what dq takes up of each row
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int p = threadIdx.x + 256 * i;
+        if (p >= P || p % W) continue;
+        float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            sum.x += piece_sum[p + j].x;
+            sum.y += piece_sum[p + j].y;
+        }
+        c.pair.row[bh * pad + blockIdx.x * 32 + p / W] = f32x4{row_own[i], sum.x, sqrtf(sum.y) * 0x1p15f, 0.0f};
     }
 }
 
@@ -200,6 +249,7 @@ void pair_layout(AttnCall *a, char *ws, bool grad)
     };
     for (int t = 0; t < kPairTensors; ++t) a->pair.img[t] = t < kPairDo || grad ? take((size_t)image_bytes(*a, t)) : nullptr;
     a->pair.scale = (float *)take((size_t)a->batch * a->kv_heads * 32);
+    a->pair.row = grad ? (f32x4 *)take((size_t)a->batch * a->kv_heads * pair_rows((int64_t)a->n * a->group) * 16) : nullptr;
     a->pair.part = (float *)take(0);
 }
 
