@@ -399,13 +399,14 @@ fs_status fs_points_release(fs_ctx *ctx);
  * read fastest).
  * FS_F32: products on the fp32 matrix cores, or, where that takes long enough (4 batch q_heads q_rows k_rows d operations, d rounded up to
  * 32, half of them under a causal line: 1.3e9 forward, 0.3e9 backward, and more than 32 rows a head of keys), from operands in two
- * fp16 pieces, summed in fp32.  They hold 22 bits of every element of q, k and v down to 2^-17 of its head's largest, of the gradient
- * d_o down to 2^-17 of its row's largest, and what is smaller to 2^-39 of that largest.  For dq gradients of scores keep 22 bits of what
- * is largest in their row.  dk, dv and dbias are sums over rows: there gradients of scores are kept to 2^-38 of the head's largest
+ * fp16 pieces, summed in fp32 ("attn_pairs" of fs_debug_set switches that off).  The pieces hold 22 bits of every element of q, k and v down
+ * to 2^-17 of its head's largest, of the gradient d_o down to 2^-17 of its row's largest, and what is smaller to 2^-39 of that
+ * largest; probabilities that meet v to 2^-29 of their row's largest or better.  For dq gradients of scores keep 22 bits of what is
+ * largest in their row.  dk, dv and dbias are sums over rows: there gradients of scores are kept to 2^-38 of the head's largest
  * |d_o_i| |v| / l_i, probabilities to 2^-40 of one, so keys that only rows of far smaller d_o see, or that no row gives a probability to
- * speak of, have gradients of fewer digits.  FS_BF16: products on the bf16 matrix cores with fp32 accumulation;
- * probabilities (2^-9 of each) and their gradients are rounded to bf16 where they enter a second product.  Maxima, sums
- * and accumulators are fp32 in both.
+ * speak of, have gradients of fewer digits.
+ * FS_BF16: products on the bf16 matrix cores with fp32 accumulation; probabilities (2^-9 of each) and their gradients are rounded to bf16
+ * where they enter a second product.  Maxima, sums and accumulators are fp32 in both.
  */
 typedef struct {
     void *data;               /* element (set 0, row 0, head 0, coordinate 0); coordinates are contiguous */

@@ -334,7 +334,7 @@ struct PairImage {
     f32x4 *row;    // of the rows of do, padded like them: the scale; <do, o> of do times 2^-15 of it; |do| times it; 0
     float *part;   // maxima of chunks of rows
 };
-constexpr float kPairP = 16.0f;      // probabilities below a reference enter the second product times this (up to 2^11: attn_slack)
+constexpr float kPairP = 16.0f;      // probabilities below a reference (up to 2^11: kSlackPair) enter the second product times this
 constexpr float kPairN = 32768.0f;   // normalised ones times this (2^15)
 
 __host__ __device__ inline int64_t pair_rows(int64_t rows) { return (rows + 127) / 128 * 128; }
