@@ -1552,7 +1552,7 @@ fs_status fs_layer_norm_grad(fs_ctx *ctx, const void *x, int32_t dtype, int64_t 
     if (!dx && !dgamma && !dbeta) return FS_OK;
     float *part = nullptr;
     if (dgamma || dbeta) {
-        if ((st = ensure_aux(c, (size_t)norm_grad_blocks(c, rows, cols, dtype) * 2 * cols * 4))) return st;
+        if ((st = ensure_aux(c, (size_t)norm_grad_part(c, rows, cols, dtype) * 4))) return st;
         part = (float *)c->aux;
     }
     return launch_norm_grad(c, x, dtype, rows, cols, ldx, gamma, wtype, stat, dy, lddy, dx, lddx, dgamma, dbeta, part);

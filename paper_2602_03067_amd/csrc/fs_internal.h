@@ -695,8 +695,8 @@ fs_status bf16_apply(Ctx *c, const Prepared *P, const Side *res, const Side *str
 void prof_begin(Ctx *c, double pairs, int kind = 0);
 void prof_end(Ctx *c);
 
-// layer norm (fs_norm.hip); part: [norm_grad_blocks][2][cols] floats where a weight's gradient is wanted
-int norm_grad_blocks(const Ctx *c, int64_t rows, int64_t cols, int32_t dtype);
+// layer norm (fs_norm.hip); part: norm_grad_part floats where a weight's gradient is wanted
+int64_t norm_grad_part(const Ctx *c, int64_t rows, int64_t cols, int32_t dtype);
 fs_status launch_norm(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, const void *beta,
                       int32_t wtype, float eps, void *y, int64_t ldy, float *stat);
 fs_status launch_norm_grad(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, int32_t wtype,

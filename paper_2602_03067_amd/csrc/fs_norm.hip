@@ -107,6 +107,7 @@ struct NormCall {
     float *stat;
     const float *stat_in;
     float *part;                // [workgroups][2][cols]
+    float *rest;                // [rows]: where rows are longer than the registers of a workgroup
     float *dgamma, *dbeta;
     int64_t rows, cols, ldx, ldy, lddy, lddx;
     float eps;
@@ -331,6 +332,19 @@ template <typename T, typename W> __global__ __launch_bounds__(kLongThreads) voi
     }
 }
 
+// what the mean of such rows, a float, is off by: the mean of the deviations
+template <typename T> __global__ __launch_bounds__(kLongThreads) void k_norm_rest_long(const NormCall c)
+{
+    __shared__ float lds[kLongThreads / 64];
+    const int64_t row = blockIdx.x;
+    const T *x = (const T *)c.x + row * c.ldx;
+    const float mean = c.stat_in[2 * row];
+    float s = 0.0f;
+    for (int64_t i = threadIdx.x; i < c.cols; i += kLongThreads) s += (float)x[i] - mean;
+    s = row_sum<kLongThreads>(s, lds) * (1.0f / (float)c.cols);
+    if (threadIdx.x == 0) c.rest[row] = s;
+}
+
 // the weights' gradients of such rows: a thread takes a column, a workgroup every blocks-th row
 template <typename T> __global__ __launch_bounds__(kNormThreads) void k_norm_wgrad_long(const NormCall c)
 {
@@ -340,7 +354,7 @@ template <typename T> __global__ __launch_bounds__(kNormThreads) void k_norm_wgr
     for (int64_t row = blockIdx.y; row < c.rows; row += c.blocks) {
         const float2 st = *(const float2 *)(c.stat_in + 2 * row);
         const float dy = (float)((const T *)c.dy)[row * c.lddy + col];
-        dg = fmaf(dy, ((float)((const T *)c.x)[row * c.ldx + col] - st.x) * st.y, dg);
+        dg = fmaf(dy, ((float)((const T *)c.x)[row * c.ldx + col] - st.x - c.rest[row]) * st.y, dg);
         db += dy;
     }
     float *out = c.part + (int64_t)blockIdx.y * 2 * c.cols;
@@ -421,7 +435,10 @@ template <typename T, typename W, int VEC> fs_status by_length(Ctx *c, const Nor
         return FS_OK;
     }
     // (dx may take dy's place: the weights' gradients first)
-    if (a.part) k_norm_wgrad_long<T><<<dim3((unsigned)ceil_div(a.cols, kNormThreads), (unsigned)a.blocks), kNormThreads, 0, c->stream>>>(a);
+    if (a.part) {
+        if (a.rows) k_norm_rest_long<T><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
+        k_norm_wgrad_long<T><<<dim3((unsigned)ceil_div(a.cols, kNormThreads), (unsigned)a.blocks), kNormThreads, 0, c->stream>>>(a);
+    }
     if (a.dx) k_norm_grad_long<T, W><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
     return FS_OK;
 }
@@ -447,12 +464,18 @@ fs_status dispatch(Ctx *c, NormCall a, int32_t dtype, int32_t wtype, bool grad)
 }  // namespace
 
 // Workgroups of a backward pass: four per CU, or as many as the rows fill.
-int norm_grad_blocks(const Ctx *c, int64_t rows, int64_t cols, int32_t dtype)
+static int norm_grad_blocks(const Ctx *c, int64_t rows, int64_t cols, int32_t dtype)
 {
     // (rows that a workgroup holds side by side, with 16-byte loads; where these cannot be used it holds no more)
     const int tpr = threads_per_row(cols, dtype == FS_BF16 ? 8 : 4);
     const int64_t fill = ceil_div(rows, tpr && tpr < kNormThreads ? kNormThreads / tpr : 1);
     return (int)std::max<int64_t>(1, std::min<int64_t>(fill, 4 * (int64_t)c->num_cu));
+}
+
+// Floats that it needs: the workgroups' shares of the weights' gradients, and of long rows what their means are off by.
+int64_t norm_grad_part(const Ctx *c, int64_t rows, int64_t cols, int32_t dtype)
+{
+    return norm_grad_blocks(c, rows, cols, dtype) * 2 * cols + (threads_per_row(cols, 1) ? 0 : rows);
 }
 
 fs_status launch_norm(Ctx *c, const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *gamma, const void *beta,
@@ -490,6 +513,7 @@ fs_status launch_norm_grad(Ctx *c, const void *x, int32_t dtype, int64_t rows, i
     a.lddy = lddy;
     a.lddx = lddx;
     a.blocks = norm_grad_blocks(c, rows, cols, dtype);
+    a.rest = part ? part + a.blocks * 2 * cols : nullptr;
     dispatch(c, a, dtype, wtype, true);
     if (a.part) k_norm_wsum<<<(unsigned)ceil_div(2 * cols, 16), 1024, 0, c->stream>>>(part, cols, a.blocks, dgamma, dbeta);
     FS_HIP(c, hipGetLastError());
