@@ -439,7 +439,7 @@ template <typename T, typename W, int VEC> fs_status by_length(Ctx *c, const Nor
         if (a.rows) k_norm_rest_long<T><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
         k_norm_wgrad_long<T><<<dim3((unsigned)ceil_div(a.cols, kNormThreads), (unsigned)a.blocks), kNormThreads, 0, c->stream>>>(a);
     }
-    if (a.dx) k_norm_grad_long<T, W><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
+    if (a.dx && a.rows) k_norm_grad_long<T, W><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
     return FS_OK;
 }
 
