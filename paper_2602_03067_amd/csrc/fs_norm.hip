@@ -100,6 +100,9 @@ template <int TPR> __device__ inline float row_sum(float v, float *lds)
     return v;
 }
 
+// 1 / sqrt(var + eps), where rounding may leave var below zero (fmaxf would make a number of NaN)
+__device__ inline float inverse_root(float var, float eps) { return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps); }
+
 struct NormCall {
     const void *x, *dy;
     const void *gamma, *beta;   // nullable
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_nor
             }
         }
     const float rest = row_sum<TPR>(s, lds[1]) * inv;
-    const float rstd = 1.0f / sqrtf(fmaxf(row_sum<TPR>(s2, lds[2]) * inv - rest * rest, 0.0f) + c.eps);
+    const float rstd = inverse_root(row_sum<TPR>(s2, lds[2]) * inv - rest * rest, c.eps);
     if (!live) return;
     T *y = (T *)c.y + row * c.ldy;
 #pragma unroll
@@ -296,7 +299,7 @@ template <typename T, typename W> __global__ __launch_bounds__(kLongThreads) voi
         s2 = fmaf(v, v, s2);
     }
     const float rest = row_sum<kLongThreads>(s, lds) * inv;
-    const float rstd = 1.0f / sqrtf(fmaxf(row_sum<kLongThreads>(s2, lds) * inv - rest * rest, 0.0f) + c.eps);
+    const float rstd = inverse_root(row_sum<kLongThreads>(s2, lds) * inv - rest * rest, c.eps);
     T *y = (T *)c.y + row * c.ldy;
     for (int64_t i = threadIdx.x; i < c.cols; i += kLongThreads) {
         float g[1], b[1];
