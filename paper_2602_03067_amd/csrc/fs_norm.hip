@@ -385,6 +385,27 @@ __global__ __launch_bounds__(1024) void k_norm_wsum(const float *part, int64_t c
     }
 }
 
+// The rows from r0 on, `rows` of them, of a call whose elements have es bytes.
+NormCall rows_from(NormCall a, int64_t r0, int64_t rows, int es)
+{
+    auto at = [&](const void *p, int64_t ld) { return p ? (char *)p + r0 * ld * es : nullptr; };
+    a.x = at(a.x, a.ldx);
+    a.y = at(a.y, a.ldy);
+    a.dy = at(a.dy, a.lddy);
+    a.dx = at(a.dx, a.lddx);
+    if (a.stat) a.stat += 2 * r0;
+    if (a.stat_in) a.stat_in += 2 * r0;
+    if (a.rest) a.rest += r0;
+    a.rows = rows;
+    return a;
+}
+// A launch has fewer than 2^32 threads: calls of more rows are several, of at most 2^31.
+template <typename F> void in_launches(const NormCall &a, int threads, int es, F launch)
+{
+    const int64_t most = (int64_t(1) << 31) / threads;
+    for (int64_t r0 = 0; r0 < a.rows; r0 += most) launch(rows_from(a, r0, std::min(most, a.rows - r0), es));
+}
+
 // Elements of a row that a thread holds at most (four arrays of them in the backward pass: with 32 among 1024 threads, which
 // have 128 registers each, they would not fit).
 constexpr int kHeld = 32, kHeldLong = 16;
@@ -400,14 +421,16 @@ int threads_per_row(int64_t cols, int vec)
 template <typename T, typename W, int VEC, int NV, int TPR> fs_status run(Ctx *c, const NormCall &a, bool grad)
 {
     constexpr int NT = TPR > kNormThreads ? TPR : kNormThreads;
-    const unsigned grid = (unsigned)(grad ? a.blocks : ceil_div(a.rows, NT / TPR));
-    if (VEC > 1 && a.past) {
-        if (grad) k_norm_grad<T, W, VEC, NV, TPR, (VEC > 1)><<<grid, NT, 0, c->stream>>>(a);
-        else k_norm<T, W, VEC, NV, TPR, (VEC > 1)><<<grid, NT, 0, c->stream>>>(a);
-    } else {
-        if (grad) k_norm_grad<T, W, VEC, NV, TPR, false><<<grid, NT, 0, c->stream>>>(a);
-        else k_norm<T, W, VEC, NV, TPR, false><<<grid, NT, 0, c->stream>>>(a);
+    if (grad) {
+        if (VEC > 1 && a.past) k_norm_grad<T, W, VEC, NV, TPR, (VEC > 1)><<<(unsigned)a.blocks, NT, 0, c->stream>>>(a);
+        else k_norm_grad<T, W, VEC, NV, TPR, false><<<(unsigned)a.blocks, NT, 0, c->stream>>>(a);
+        return FS_OK;
     }
+    in_launches(a, TPR, sizeof(T), [&](const NormCall &p) {
+        const unsigned grid = (unsigned)ceil_div(p.rows, NT / TPR);
+        if (VEC > 1 && p.past) k_norm<T, W, VEC, NV, TPR, (VEC > 1)><<<grid, NT, 0, c->stream>>>(p);
+        else k_norm<T, W, VEC, NV, TPR, false><<<grid, NT, 0, c->stream>>>(p);
+    });
     return FS_OK;
 }
 
@@ -434,15 +457,16 @@ template <typename T, typename W, int VEC> fs_status by_length(Ctx *c, const Nor
     case kLongThreads: return run<T, W, VEC, kHeldLong / VEC, kLongThreads>(c, a, grad);
     }
     if (!grad) {
-        k_norm_long<T, W><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
+        in_launches(a, kLongThreads, sizeof(T), [&](const NormCall &p) { k_norm_long<T, W><<<(unsigned)p.rows, kLongThreads, 0, c->stream>>>(p); });
         return FS_OK;
     }
     // (dx may take dy's place: the weights' gradients first)
     if (a.part) {
-        if (a.rows) k_norm_rest_long<T><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
+        in_launches(a, kLongThreads, sizeof(T), [&](const NormCall &p) { k_norm_rest_long<T><<<(unsigned)p.rows, kLongThreads, 0, c->stream>>>(p); });
         k_norm_wgrad_long<T><<<dim3((unsigned)ceil_div(a.cols, kNormThreads), (unsigned)a.blocks), kNormThreads, 0, c->stream>>>(a);
     }
-    if (a.dx && a.rows) k_norm_grad_long<T, W><<<(unsigned)a.rows, kLongThreads, 0, c->stream>>>(a);
+    if (a.dx)
+        in_launches(a, kLongThreads, sizeof(T), [&](const NormCall &p) { k_norm_grad_long<T, W><<<(unsigned)p.rows, kLongThreads, 0, c->stream>>>(p); });
     return FS_OK;
 }
 
