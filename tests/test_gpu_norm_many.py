@@ -26,13 +26,15 @@ def test_half_a_billion_short_rows():
     def check(y, stat, x):
         h = (x[:, 0].double() - x[:, 1].double()) / 2
         want = h / (h * h + 1e-5).sqrt()
-        assert ((y[:, 0].double() - want).abs() <= 2.0 ** -8 * want.abs()).all() and ((y[:, 1].double() + want).abs() <= 2.0 ** -8 * want.abs()).all()
-        assert ((stat[:, 0].double() - x.double().mean(1)).abs() <= 1e-6 * x.double().abs().amax(1)).all()
+        near = bool(((y[:, 0].double() - want).abs() <= 2.0 ** -8 * want.abs()).all() and ((y[:, 1].double() + want).abs() <= 2.0 ** -8 * want.abs()).all())
+        mean = bool(((stat[:, 0].double() - x.double().mean(1)).abs() <= 1e-6 * x.double().abs().amax(1)).all())
+        assert near and mean
 
     check(y[:1 << 20], stat[:1 << 20], some)
     for k in range(1, 512):
         at = slice(k << 20, (k + 1) << 20)
-        assert torch.equal(y[at], y[:1 << 20]) and torch.equal(stat[at], stat[:1 << 20]), k
+        same = torch.equal(y[at], y[:1 << 20]) and torch.equal(stat[at], stat[:1 << 20])
+        assert same, k
     check(y[1 << 29:], stat[1 << 29:], x[1 << 29:])
     ctx.close()
     del x, y, stat
