@@ -18,6 +18,7 @@ namespace {
 constexpr int kAdamBlock = 256;     // weights under one scale; 64 lanes, four each
 constexpr int kAdamChunk = 1024;    // weights of a workgroup: four waves, a block each
 constexpr int kTableBytes = 3840;   // of a launch's 4 KB of arguments
+constexpr int64_t kLaunchChunks = 1 << 23;   // workgroups of a launch, which has fewer than 2^32 threads: what is left of a tensor goes on in the next
 
 enum { kP, kG, kM, kV, kMaster, kMs, kVs, kSlots };
 
@@ -242,30 +243,33 @@ fs_status run(Ctx *c, const AdamStep &s, const fs_adamw_tensor *t, int32_t count
 {
     using S = Slots<MASTER, Q8>;
     uint32_t block = 0;
+    int64_t done = 0;   // weights of tensor k that earlier launches have: whole workgroups
     for (int32_t k = 0; k < count;) {
         Table<MASTER, Q8> tb;
         int64_t chunks = 0;
         tb.count = 0;
-        for (; k < count && tb.count < Table<MASTER, Q8>::kMost; ++k) {
-            const int64_t mine = ceil_div(t[k].n, kAdamChunk);
-            if (mine == 0) continue;
-            if (chunks + mine > INT32_MAX) break;   // (a tensor has fewer: checked by the caller)
-            const int q = tb.count++;
-            void **at = tb.at[q];
-            at[S::of(kP)] = t[k].p;
-            at[S::of(kG)] = const_cast<void *>(t[k].g);
-            at[S::of(kM)] = t[k].m;
-            at[S::of(kV)] = t[k].v;
-            if constexpr (MASTER) at[S::of(kMaster)] = t[k].master;
-            if constexpr (Q8) {
-                at[S::of(kMs)] = t[k].m_scale;
-                at[S::of(kVs)] = t[k].v_scale;
+        while (k < count && tb.count < Table<MASTER, Q8>::kMost && chunks < kLaunchChunks) {
+            const int64_t left = t[k].n - done, n = std::min(left, (kLaunchChunks - chunks) * kAdamChunk), mine = ceil_div(n, kAdamChunk);
+            if (mine) {
+                const int q = tb.count++;
+                void **at = tb.at[q];
+                at[S::of(kP)] = (P *)t[k].p + done;
+                at[S::of(kG)] = (G *)const_cast<void *>(t[k].g) + done;
+                at[S::of(kM)] = (char *)t[k].m + done * (Q8 ? 1 : 4);
+                at[S::of(kV)] = (char *)t[k].v + done * (Q8 ? 1 : 4);
+                if constexpr (MASTER) at[S::of(kMaster)] = t[k].master + done;
+                if constexpr (Q8) {
+                    at[S::of(kMs)] = t[k].m_scale + done / kAdamBlock;
+                    at[S::of(kVs)] = t[k].v_scale + done / kAdamBlock;
+                }
+                tb.n[q] = n;
+                tb.chunk[q] = (int32_t)chunks;
+                tb.block[q] = block;
+                chunks += mine;
+                block += (uint32_t)ceil_div(n, kAdamBlock);
             }
-            tb.n[q] = t[k].n;
-            tb.chunk[q] = (int32_t)chunks;
-            tb.block[q] = block;
-            chunks += mine;
-            block += (uint32_t)ceil_div(t[k].n, kAdamBlock);
+            done = n < left ? done + n : 0;
+            if (n == left) ++k;
         }
         if (tb.count) k_adamw<P, G, MASTER, Q8><<<(unsigned)chunks, 256, 0, c->stream>>>(tb, s);
     }
