@@ -647,6 +647,13 @@ fs_status check_attn(Ctx *c, AttnCheck *k, const fs_attn *a, AttnCall *call)
     return FS_OK;
 }
 
+// A launch has fewer than 2^32 threads; more of them are not an error to the runtime, which then starts too few workgroups.
+fs_status check_launch(Ctx *c, int64_t workgroups, int threads)
+{
+    if (workgroups < (int64_t(1) << 32) / threads) return FS_OK;
+    return fail(c, FS_ERR_BAD_SHAPE, "too many sets, heads and rows for one call");
+}
+
 fs_status check_stat(Ctx *c, const float *stat, int64_t rows)
 {
     if (!rows) return FS_OK;
@@ -1424,13 +1431,14 @@ fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, floa
     if ((st = check_stat(c, stat, rows))) return st;
     for (int i = 0; i < k.n_in; ++i)
         if (overlap(stat, (size_t)rows * 8, k.in[i].p, k.in[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "stat overlaps an input");
-    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
-    if (!rows) return FS_OK;
     a.o = o->data;
     a.so = {o->batch, o->row, o->head};
     a.stat = stat;
     const bool f32 = attn->dtype == FS_F32;
-    const AttnPlan p = attn_plan(c, a, f32);
+    const AttnPlan p = rows ? attn_plan(c, a, f32) : AttnPlan();
+    if ((st = check_launch(c, p.grid, p.threads))) return st;
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!rows) return FS_OK;
     a.splits = p.splits;
     if (p.splits > 1 || p.pairs) {
         Arena A;
@@ -1472,8 +1480,6 @@ fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o,
             if (overlap(dbias, rows_bytes(attn->batch, attn->k_rows, dbias_ld, k.es), k.in[i].p, k.in[i].bytes))
                 return fail(c, FS_ERR_INVALID_ARG, "dbias overlaps an input");
     }
-    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
-    if (!attn->batch) return FS_OK;
     a.o = o->data;
     a.so = {o->batch, o->row, o->head};
     a.d_o = d_o->data;
@@ -1488,7 +1494,10 @@ fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o,
     a.dbias = dbias;
     a.dbias_ld = dbias_ld;
     const bool f32 = attn->dtype == FS_F32;
-    const AttnGradPlan p = attn_grad_plan(c, a, f32);
+    const AttnGradPlan p = attn->batch ? attn_grad_plan(c, a, f32) : AttnGradPlan();
+    if ((st = check_launch(c, std::max(p.q_grid, p.k_grid), 256))) return st;
+    if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
+    if (!attn->batch) return FS_OK;
     Arena A;
     A.take(p.stat_bytes);
     A.take(p.dq_bytes);

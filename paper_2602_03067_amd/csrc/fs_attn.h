@@ -422,20 +422,20 @@ fs_status launch_pairs(Ctx *c, const AttnCall &a, bool grad, bool aligned);
 
 // how a forward pass is launched
 struct AttnPlan {
-    int rows, splits;   // packed rows of a workgroup
-    bool pairs;
-    int64_t grid;
-    size_t part_bytes, stat_bytes, pair_bytes;
+    int rows = 0, splits = 1, threads = 64;   // packed rows and threads of a workgroup
+    bool pairs = false;
+    int64_t grid = 0;
+    size_t part_bytes = 0, stat_bytes = 0, pair_bytes = 0;
 };
 AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32);
 fs_status launch_attn(Ctx *c, const AttnCall &a, const AttnPlan &p, bool f32, bool aligned);
 
 // ... and a backward pass: rows' side (dq) and keys' side (dk, dv)
 struct AttnGradPlan {
-    int q_splits, k_splits;
-    bool pairs;
-    int64_t q_grid, k_grid;
-    size_t stat_bytes, dq_bytes, dkv_bytes, dbias_bytes, pair_bytes;
+    int q_splits = 1, k_splits = 1;
+    bool pairs = false;
+    int64_t q_grid = 0, k_grid = 0;
+    size_t stat_bytes = 0, dq_bytes = 0, dkv_bytes = 0, dbias_bytes = 0, pair_bytes = 0;
 };
 AttnGradPlan attn_grad_plan(const Ctx *c, const AttnCall &a, bool f32);
 // `ws`: the bytes of the plan, each piece rounded up to 256

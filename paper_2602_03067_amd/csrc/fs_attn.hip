@@ -437,6 +437,7 @@ AttnPlan attn_plan(const Ctx *c, const AttnCall &a, bool f32)
     // a few queries over long keys, which is bound by memory.
     const int64_t wide = ceil_div(rows, 128) * heads, few = few_keys((int)round_up(a.d, 32));
     p.rows = p.pairs ? 128 : rows <= 32 ? 32 : !f32 && wide < c->num_cu && a.m >= few ? 64 : 128;
+    p.threads = p.rows == 32 ? 64 : p.rows == 64 ? 512 : 256;
     const int64_t kt = p.rows == 64 ? few : p.rows == 32 || f32 ? 32 : 64;
     const int64_t blocks = ceil_div(rows, p.rows) * heads, tiles = ceil_div(a.m, kt);
     const int64_t want = (int64_t)c->num_cu * (p.rows == 32 ? 4 : p.rows == 64 ? 1 : 2);

@@ -227,7 +227,7 @@ int64_t image_bytes(const AttnCall &a, int tensor)
 bool pair_worth(const Ctx *c, const AttnCall &a, bool grad)
 {
     const int64_t rows = (int64_t)a.n * a.group;
-    if (rows == 0 || a.m == 0 || (int64_t)a.batch * a.kv_heads > 65535) return false;
+    if (rows == 0 || a.m == 0 || (int64_t)a.batch * a.kv_heads > 65535 || rows > int64_t(1) << 28) return false;   // (what the two passes' grids hold)
     if (c->dbg_attn_pairs) return c->dbg_attn_pairs == 1;
     return rows > 32 && 4.0 * (double)a.batch * a.kv_heads * rows * a.m * round_up(a.d, 32) * (a.causal ? 0.5 : 1.0) >= (grad ? 0.3e9 : 1.3e9);
 }

@@ -1,0 +1,49 @@
+"""Sizes that the operators' launches do not hold are refused, through a host-only context."""
+import ctypes
+
+import pytest
+
+from paper_2602_03067_amd import binding
+from paper_2602_03067_amd.binding import FsAttn, FsHeads
+
+OK_ON_HOST, SHAPE = 7, 2
+TB = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return binding.load_library()
+
+
+@pytest.fixture()
+def hctx(lib):
+    h = ctypes.c_void_p()
+    assert lib.fs_create(ctypes.byref(h), -1, None) == 0
+    yield h
+    lib.fs_destroy(h)
+
+
+def call(batch, n, m, heads, kv_heads, d, dtype=1):
+    """Tensors of a TB each, one behind the other."""
+    q, kv = (n * heads * d, heads * d, d), (m * kv_heads * d, kv_heads * d, d)
+    at = [FsHeads((1 + i) * TB, *(kv if i in (1, 2, 6, 7) else q)) for i in range(8)]
+    q, k, v, o, do, dq, dk, dv = at
+    kw = FsAttn(q, k, v, dtype, 0, batch, n, m, heads, kv_heads, d, 0.25, None, None, None, 0)
+    return kw, [ctypes.byref(x) for x in (o, do, dq, dk, dv)]
+
+
+@pytest.mark.parametrize("batch,n,m,heads,kv_heads,d,forward,backward", [
+    (1 << 20, 1, 40, 16, 16, 8, OK_ON_HOST, SHAPE),          # 2^24 heads of keys: 64 threads each forward, 256 backward
+    ((1 << 20) - 1, 1, 40, 16, 16, 8, OK_ON_HOST, OK_ON_HOST),
+    (1 << 22, 1, 40, 16, 16, 8, SHAPE, SHAPE),               # 2^26
+    ((1 << 22) - 1, 1, 40, 16, 16, 8, OK_ON_HOST, SHAPE),
+    (1 << 22, 1, 40, 64, 16, 8, SHAPE, SHAPE),
+    (1 << 20, 200, 40, 8, 8, 8, SHAPE, SHAPE),               # two workgroups of 256 threads a head
+    (1 << 20, 200, 40, 4, 4, 8, OK_ON_HOST, OK_ON_HOST),
+    (1 << 20, 1, 200, 8, 8, 8, OK_ON_HOST, SHAPE),
+    (1, 1 << 24, 1 << 20, 64, 1, 8, OK_ON_HOST, OK_ON_HOST),
+])
+def test_attention(lib, hctx, batch, n, m, heads, kv_heads, d, forward, backward):
+    a, (o, do, dq, dk, dv) = call(batch, n, m, heads, kv_heads, d)
+    assert lib.fs_attention(hctx, ctypes.byref(a), o, 9 * TB) == forward
+    assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, dv, None, 0) == backward
