@@ -425,11 +425,12 @@ typedef struct {
     int64_t bias_ld;                  /* elements from one set's bias to the next, >= k_rows or 0 (shared)        */
 } fs_attn;
 
-/* o: written, q's shape (strides >= d); stat: [batch][q_heads][q_rows][2] floats, aligned to 8 bytes, receives (m_i, l_i). */
+/* o: written, q's shape (its strides nest, each at least the extent of what lies within it, so that no rows meet);
+ * stat: [batch][q_heads][q_rows][2] floats, aligned to 8 bytes, receives (m_i, l_i). */
 fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, float *stat /* device */);
 
 /*
- * Gradients of fs_attention for the gradient d_o of its output: dq, dk, dv (q's, k's and v's shapes, all written; summed
+ * Gradients of fs_attention for the gradient d_o of its output: dq, dk, dv (q's, k's and v's shapes, strides that nest, all written; summed
  * over the heads that share keys), and dbias [batch][k_rows] of `dtype` (stride dbias_ld >= k_rows, at most 65535 sets), NULL to skip.  o and
  * stat are what fs_attention gave.  The probabilities are computed anew from stat; no n x m matrix is stored.
  */

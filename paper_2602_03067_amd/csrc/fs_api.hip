@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 #include <new>
 
@@ -585,10 +586,19 @@ fs_status check_heads(Ctx *c, AttnCheck *k, const fs_heads *t, bool kv, bool out
     for (int i = 0; i < 3; ++i) {
         if (stride[i] < 0 || stride[i] > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "%s: a stride is negative or beyond 2^40", name);
         if (count[i] <= 1) continue;
-        if (out && stride[i] < a->d) return fail(c, FS_ERR_BAD_SHAPE, "%s: rows of an output overlap", name);
         aligned = aligned && stride[i] * k->es % 16 == 0;
     }
     k->aligned = k->aligned && aligned;
+    if (out) {   // the strides nest: from the smallest on each is at least what lies within it
+        int order[3] = {0, 1, 2};
+        std::sort(order, order + 3, [&](int x, int y) { return stride[x] < stride[y]; });
+        int64_t within = a->d;
+        for (int i : order) {
+            if (count[i] <= 1) continue;
+            if (stride[i] < within) return fail(c, FS_ERR_BAD_SHAPE, "%s: rows of an output overlap", name);
+            within += (count[i] - 1) * stride[i];
+        }
+    }
     const size_t bytes = (size_t)heads_span(*t, a->batch, rows, heads, a->d) * k->es;
     if (!out) {
         k->in[k->n_in++] = {t->data, bytes};

@@ -1,4 +1,4 @@
-"""Sizes that the operators' launches do not hold are refused, through a host-only context."""
+"""Sizes that the operators' launches do not hold, and outputs whose parts meet, are refused, through a host-only context."""
 import ctypes
 
 import pytest
@@ -47,3 +47,18 @@ def test_attention(lib, hctx, batch, n, m, heads, kv_heads, d, forward, backward
     a, (o, do, dq, dk, dv) = call(batch, n, m, heads, kv_heads, d)
     assert lib.fs_attention(hctx, ctypes.byref(a), o, 9 * TB) == forward
     assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, dv, None, 0) == backward
+
+
+@pytest.mark.parametrize("strides,status", [
+    ((4 * 8 * 16, 8 * 16, 16), OK_ON_HOST), ((8 * 4 * 16, 16, 4 * 16), OK_ON_HOST),      # rows first, heads first
+    ((3 * 4 * 8 * 16, 3 * 8 * 16, 16), OK_ON_HOST), ((16, 2 * 8 * 16, 2 * 16), OK_ON_HOST),   # inside a projection's, sets innermost
+    ((16, 16, 16), SHAPE), ((4 * 8 * 16, 16, 16), SHAPE), ((4 * 8 * 16, 8 * 16, 17), SHAPE), ((4 * 8 * 16, 8 * 16 - 1, 16), SHAPE),
+    ((4 * 8 * 16 - 16, 8 * 16, 16), SHAPE), ((8 * 4 * 16, 16, 4 * 16 - 8), SHAPE), ((0, 8 * 16, 16), SHAPE), ((8 * 16, 4 * 8 * 16, 16), OK_ON_HOST), ((8 * 16, 2 * 8 * 16 - 16, 16), SHAPE),
+])
+def test_rows_of_an_output_do_not_meet(lib, hctx, strides, status):
+    """Two sets of four rows, eight heads of 16."""
+    a, (o, do, dq, dk, dv) = call(2, 4, 4, 8, 8, 16)
+    out = ctypes.byref(FsHeads(10 * TB, *strides))
+    assert lib.fs_attention(hctx, ctypes.byref(a), out, 9 * TB) == status
+    assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, out, dk, dv, None, 0) == status
+    assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, out, None, 0) == status
