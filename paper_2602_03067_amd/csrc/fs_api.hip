@@ -569,9 +569,19 @@ struct AttnCheck {
     struct Span {
         const void *p;
         size_t bytes;
-    } in[8];
-    int n_in = 0;
+    } in[10], out[4];
+    int n_in = 0, n_out = 0;
 };
+
+// an output against all inputs, and against the outputs before it
+fs_status check_apart(Ctx *c, AttnCheck *k, const void *p, size_t bytes, const char *name)
+{
+    for (int i = 0; i < k->n_in; ++i)
+        if (overlap(p, bytes, k->in[i].p, k->in[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "%s overlaps an input", name);
+    for (int i = 0; i < k->n_out; ++i)
+        if (overlap(p, bytes, k->out[i].p, k->out[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "%s overlaps another output", name);
+    return FS_OK;
+}
 
 fs_status check_heads(Ctx *c, AttnCheck *k, const fs_heads *t, bool kv, bool out, const char *name)
 {
@@ -605,6 +615,10 @@ fs_status check_heads(Ctx *c, AttnCheck *k, const fs_heads *t, bool kv, bool out
     } else {
         for (int i = 0; i < k->n_in; ++i)
             if (overlap(t->data, bytes, k->in[i].p, k->in[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "%s overlaps an input", name);
+        // (dq, dk and dv may be parts of one buffer, row by row; they do not begin at one place)
+        for (int i = 0; i < k->n_out; ++i)
+            if (bytes && t->data == k->out[i].p) return fail(c, FS_ERR_INVALID_ARG, "%s overlaps another output", name);
+        k->out[k->n_out++] = {t->data, bytes};
     }
     return FS_OK;
 }
@@ -633,6 +647,8 @@ fs_status check_attn(Ctx *c, AttnCheck *k, const fs_attn *a, AttnCall *call)
         (st = check_heads(c, k, &a->v, true, false, "v")))
         return st;
     if (a->bias && a->batch) k->in[k->n_in++] = {a->bias, (size_t)((a->batch - 1) * a->bias_ld + a->k_rows) * 4};
+    k->in[k->n_in++] = {a->q_len, (size_t)a->batch * 4};
+    k->in[k->n_in++] = {a->k_len, (size_t)a->batch * 4};
     auto at = [](const fs_heads &t) { return HeadsAt{t.batch, t.row, t.head}; };
     *call = AttnCall();
     call->q = a->q.data;
@@ -1439,8 +1455,7 @@ fs_status fs_attention(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o, floa
     if ((st = check_attn(c, &k, attn, &a)) || (st = check_heads(c, &k, o, false, true, "o"))) return st;
     const int64_t rows = attn->batch * attn->q_heads * attn->q_rows;
     if ((st = check_stat(c, stat, rows))) return st;
-    for (int i = 0; i < k.n_in; ++i)
-        if (overlap(stat, (size_t)rows * 8, k.in[i].p, k.in[i].bytes)) return fail(c, FS_ERR_INVALID_ARG, "stat overlaps an input");
+    if ((st = check_apart(c, &k, stat, (size_t)rows * 8, "stat"))) return st;
     a.o = o->data;
     a.so = {o->batch, o->row, o->head};
     a.stat = stat;
@@ -1486,9 +1501,7 @@ fs_status fs_attention_grad(fs_ctx *ctx, const fs_attn *attn, const fs_heads *o,
         if (attn->bias_ld == 0 && attn->batch > 1) return fail(c, FS_ERR_UNSUPPORTED, "dbias of a bias that the sets share");
         if (dbias_ld < attn->k_rows || dbias_ld > (int64_t(1) << 40)) return fail(c, FS_ERR_BAD_SHAPE, "dbias_ld is smaller than k_rows, or beyond 2^40");
         if ((uintptr_t)dbias % k.es) return fail(c, FS_ERR_INVALID_ARG, "dbias is not aligned to its type");
-        for (int i = 0; i < k.n_in; ++i)
-            if (overlap(dbias, rows_bytes(attn->batch, attn->k_rows, dbias_ld, k.es), k.in[i].p, k.in[i].bytes))
-                return fail(c, FS_ERR_INVALID_ARG, "dbias overlaps an input");
+        if ((st = check_apart(c, &k, dbias, rows_bytes(attn->batch, attn->k_rows, dbias_ld, k.es), "dbias"))) return st;
     }
     a.o = o->data;
     a.so = {o->batch, o->row, o->head};
@@ -1539,6 +1552,7 @@ fs_status fs_layer_norm(fs_ctx *ctx, const void *x, int32_t dtype, int64_t rows,
     for (const auto &i : in)
         if (overlap(y, rows_bytes(rows, cols, ldy, es), i.p, i.bytes) || overlap(stat, (size_t)rows * 8, i.p, i.bytes))
             return fail(c, FS_ERR_INVALID_ARG, "an output overlaps an input");
+    if (overlap(y, rows_bytes(rows, cols, ldy, es), stat, (size_t)rows * 8)) return fail(c, FS_ERR_INVALID_ARG, "y overlaps stat");
     if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
     if (!rows) return FS_OK;
     return launch_norm(c, x, dtype, rows, cols, ldx, gamma, beta, wtype, eps, y, ldy, stat);
@@ -1567,6 +1581,9 @@ fs_status fs_layer_norm_grad(fs_ctx *ctx, const void *x, int32_t dtype, int64_t 
         for (const auto &q : out)
             if (overlap(q.p, q.bytes, i.p, i.bytes) && !(in_place && q.p == dx && i.p == dy))
                 return fail(c, FS_ERR_INVALID_ARG, "an output overlaps an input");
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return fail(c, FS_ERR_INVALID_ARG, "an output overlaps another output");
     if (c->device < 0) return fail(c, FS_ERR_DEVICE, "%s", kHostOnly);
     if (!dx && !dgamma && !dbeta) return FS_OK;
     float *part = nullptr;

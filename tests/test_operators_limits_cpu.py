@@ -1,4 +1,4 @@
-"""Sizes that the operators' launches do not hold, and outputs whose parts meet, are refused, through a host-only context."""
+"""Sizes that the operators' launches do not hold, and outputs that meet, are refused, through a host-only context."""
 import ctypes
 
 import pytest
@@ -6,7 +6,7 @@ import pytest
 from paper_2602_03067_amd import binding
 from paper_2602_03067_amd.binding import FsAttn, FsHeads
 
-OK_ON_HOST, SHAPE = 7, 2
+OK_ON_HOST, INVALID, SHAPE = 7, 1, 2
 TB = 1 << 40
 
 
@@ -62,3 +62,48 @@ def test_rows_of_an_output_do_not_meet(lib, hctx, strides, status):
     assert lib.fs_attention(hctx, ctypes.byref(a), out, 9 * TB) == status
     assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, out, dk, dv, None, 0) == status
     assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, out, None, 0) == status
+
+
+def test_outputs_of_attention_do_not_meet(lib, hctx):
+    a, (o, do, dq, dk, dv) = call(2, 4, 4, 8, 8, 16)
+    size = 2 * 4 * 8 * 16 * 2
+    assert lib.fs_attention(hctx, ctypes.byref(a), o, 9 * TB) == OK_ON_HOST
+    for stat in (4 * TB, 4 * TB + size - 8, 4 * TB - 8):
+        assert lib.fs_attention(hctx, ctypes.byref(a), o, stat) == INVALID
+    assert lib.fs_attention(hctx, ctypes.byref(a), o, 4 * TB + size) == OK_ON_HOST
+
+    def backward(dq, dk, dv, db=None, a=a):
+        return lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, dv, db, 4 if db else 0)
+
+    assert backward(dq, dk, dv) == OK_ON_HOST
+    assert backward(dq, dq, dv) == INVALID and backward(dq, dk, dk) == INVALID and backward(dv, dk, dv) == INVALID
+    a.bias, a.bias_ld = 11 * TB, 4
+    assert backward(dq, dk, dv, 12 * TB) == OK_ON_HOST
+    for at in (6, 7, 8):
+        assert backward(dq, dk, dv, at * TB) == INVALID
+
+
+def test_outputs_of_attention_are_not_its_lengths(lib, hctx):
+    a, (o, do, dq, dk, dv) = call(2, 4, 4, 8, 8, 16)
+    for field in ("q_len", "k_len"):
+        setattr(a, field, 9 * TB + 64)
+        assert lib.fs_attention(hctx, ctypes.byref(a), o, 9 * TB) == INVALID
+        setattr(a, field, 6 * TB + 64)
+        assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, dv, None, 0) == INVALID
+        setattr(a, field, 13 * TB)
+        assert lib.fs_attention(hctx, ctypes.byref(a), o, 9 * TB) == OK_ON_HOST
+        assert lib.fs_attention_grad(hctx, ctypes.byref(a), o, 9 * TB, do, dq, dk, dv, None, 0) == OK_ON_HOST
+
+
+def test_outputs_of_layer_norm_do_not_meet(lib, hctx):
+    def forward(y, stat):
+        return lib.fs_layer_norm(hctx, TB, 0, 4, 8, 8, None, None, 0, 1e-5, y, 8, stat)
+
+    assert forward(2 * TB, 2 * TB + 128) == OK_ON_HOST and forward(2 * TB, 2 * TB + 120) == INVALID and forward(2 * TB + 24, 2 * TB) == INVALID
+
+    def backward(dx, dgamma, dbeta):
+        return lib.fs_layer_norm_grad(hctx, TB, 0, 4, 8, 8, None, 0, 3 * TB, 4 * TB, 8, dx, 8, dgamma, dbeta)
+
+    assert backward(5 * TB, 5 * TB + 128, 5 * TB + 160) == OK_ON_HOST
+    assert backward(5 * TB, 5 * TB + 124, None) == INVALID and backward(5 * TB, None, 5 * TB + 64) == INVALID
+    assert backward(None, 6 * TB, 6 * TB + 28) == INVALID and backward(4 * TB, 6 * TB, 4 * TB + 100) == INVALID
