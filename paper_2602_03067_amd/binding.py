@@ -530,7 +530,8 @@ class AdamW:
 
     ``state_bits`` 8 keeps m and sqrt(v) as float8 codes under a scale for every 256 weights.  ``master``: float copies of bf16
     weights.  The state is made here unless it is given (``m``, ``v``, ``m_scale``, ``v_scale``, and ``step``, the steps already taken);
-    its tensors and the master copies stay the ones of the beginning: another state is copied into them.
+    its tensors and the master copies stay the ones of the beginning: another state is copied into them.  A weight may be given
+    other memory between steps, of the same size and type; what it had before is kept until the next step.
     """
 
     def __init__(self, ctx: Context, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
@@ -575,6 +576,9 @@ class AdamW:
             entry.n = n
         self._at = np.frombuffer(self._table, dtype=np.int64).reshape(len(self.params), 8)   # (the table's addresses: p, g, ...)
         self._p_at = list(map(torch.Tensor.data_ptr, self.params))
+        # The memory behind the table's addresses lives as long as they are in it, whatever the tensors are made to point to meanwhile:
+        # so no other tensor has an address of the table, and a weight at its address is the weight that was checked.
+        self._held = [t.detach() for tensors, _ in lists for t in tensors or ()]
         self._args = FsAdamwArgs(p_dtype=_DTYPES[self.p_dtype], state_bits=state_bits)
 
     def _check_params(self):
@@ -602,6 +606,7 @@ class AdamW:
                 raise ValueError("a weight changed its size")
             self._p_at = p_at
             self._at[:, 0] = p_at
+            self._held[:len(p_at)] = [p.detach() for p in self.params]
         a = self._args
         a.lr, (a.beta1, a.beta2), a.eps, a.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
         a.step, a.g_dtype = self.step_count + 1, _DTYPES[kind]
