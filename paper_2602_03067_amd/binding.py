@@ -575,6 +575,10 @@ class AdamW:
         for entry, n in zip(self._table, self._sizes):
             entry.n = n
         self._at = np.frombuffer(self._table, dtype=np.int64).reshape(len(self.params), 8)   # (the table's addresses: p, g, ...)
+        wide = [p.element_size() for p in self.params]
+        self._bytes = np.array([(n * w, n * 4 * (self.master is not None), *((n, n, (n + 255) // 256 * 4, (n + 255) // 256 * 4) if state_bits == 8 else
+                                                                           (n * 4, n * 4, 0, 0))) for n, w in zip(self._sizes, wide)], dtype=np.int64)
+        self._check_apart()
         self._p_at = list(map(torch.Tensor.data_ptr, self.params))
         # The memory behind the table's addresses lives as long as they are in it, whatever the tensors are made to point to meanwhile:
         # so no other tensor has an address of the table, and a weight at its address is the weight that was checked.
@@ -585,6 +589,14 @@ class AdamW:
         for p in self.params:
             if not p.is_cuda or p.dtype != self.p_dtype or not p.is_contiguous():
                 raise TypeError("weights must be contiguous GPU tensors of one type")
+
+    def _check_apart(self):
+        """What a step writes does not overlap: a weight given twice, or one state for two, would be updated by two at once."""
+        first, size = self._at[:, [0, 2, 3, 4, 5, 6]].ravel(), self._bytes.ravel()   # p, master, m, v, m_scale, v_scale
+        first, size = first[size > 0], size[size > 0]
+        order = np.argsort(first)
+        if (first[order][:-1] + size[order][:-1] > first[order][1:]).any():
+            raise ValueError("weights or states overlap each other")
 
     def step(self, grads, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step with these gradients (one type, contiguous, in the order of the weights).  ``grad_scale``: a float32 GPU scalar
@@ -604,8 +616,14 @@ class AdamW:
             self._check_params()
             if list(map(torch.Tensor.numel, self.params)) != self._sizes:
                 raise ValueError("a weight changed its size")
-            self._p_at = p_at
+            before = self._at[:, 0].copy()
             self._at[:, 0] = p_at
+            try:
+                self._check_apart()
+            except ValueError:
+                self._at[:, 0] = before
+                raise
+            self._p_at = p_at
             self._held[:len(p_at)] = [p.detach() for p in self.params]
         a = self._args
         a.lr, (a.beta1, a.beta2), a.eps, a.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
