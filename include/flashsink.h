@@ -385,6 +385,10 @@ fs_status fs_points_release(fs_ctx *ctx);
  * owned by the caller, work enqueued on the context's stream, status codes) and use the context's second buffer for
  * partial results, so copies that fs_points_keep declares stay.  None of them synchronises, but for a call that has to grow
  * that buffer.  Nothing is added by atomics: results do not depend on the order in which workgroups run.
+ * Recorded into a graph they hold their arguments as they were (fs_adamw: step and seed too, so every replay repeats one bias correction
+ * and, with 8-bit state, one rounding, whose codes then are right on average over weights and no longer over steps), and the second
+ * buffer, which then stays until fs_destroy.  It cannot grow while a graph is recorded (FS_ERR_ALLOC): make a call of that size once
+ * before.
  */
 
 /*

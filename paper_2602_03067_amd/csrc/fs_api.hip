@@ -533,13 +533,26 @@ fs_status grad_common(Ctx *c, const fs_problem *prob, float eps, const float *f,
                                 wrt_y ? prob->b : prob->a, mass, mode);
 }
 
-// the context's second buffer (kept across the entry points that lay the workspace out anew), at least `need` bytes
+// the context's second buffer (kept across the entry points that lay the workspace out anew), at least `need` bytes.  One that a graph has
+// recorded is kept until fs_destroy, also when a larger one takes its place.
 fs_status ensure_aux(Ctx *c, size_t need)
 {
-    if (need <= c->aux_bytes) return FS_OK;
+    const bool recorded = capturing(c);
+    if (need <= c->aux_bytes) {
+        c->aux_recorded |= recorded;
+        return FS_OK;
+    }
+    if (recorded) return fail(c, FS_ERR_ALLOC, "the context's second buffer cannot grow while a graph is recorded: make such a call once before");
     FS_HIP(c, hipStreamSynchronize(c->stream));
     if (c->aux) {
-        FS_HIP(c, hipFree(c->aux));
+        if (c->aux_recorded) {
+            KeptBuffer *kept = new (std::nothrow) KeptBuffer{c->aux, c->aux_kept};
+            if (!kept) return fail(c, FS_ERR_ALLOC, "no host memory");
+            c->aux_kept = kept;
+        } else {
+            FS_HIP(c, hipFree(c->aux));
+        }
+        c->aux_recorded = false;
         c->aux = nullptr;
         c->aux_bytes = 0;
     }
@@ -792,6 +805,11 @@ fs_status fs_destroy(fs_ctx *ctx)
         for (hipEvent_t e : c->ev_pool) (void)hipEventDestroy(e);
         if (c->ws) (void)hipFree(c->ws);
         if (c->aux) (void)hipFree(c->aux);
+        while (KeptBuffer *kept = c->aux_kept) {
+            (void)hipFree(kept->at);
+            c->aux_kept = kept->next;
+            delete kept;
+        }
         if (c->fx_count) (void)hipFree(c->fx_count);
         if (c->pin) (void)hipHostFree(c->pin);
         if (c->box) (void)hipHostFree(c->box);

@@ -195,6 +195,12 @@ struct Splits {
     Splits(int n_ = 1, int alt_ = 0) : n(n_), alt(alt_) {}
 };
 
+// a buffer that outlives its use, until fs_destroy
+struct KeptBuffer {
+    char *at;
+    KeptBuffer *next;
+};
+
 // ---------------------------------------------------------------------------------------
 // context
 // ---------------------------------------------------------------------------------------
@@ -211,6 +217,8 @@ struct Ctx {
     // grow-only second buffer for entry points that call other entry points (which lay the workspace out anew)
     char *aux = nullptr;
     size_t aux_bytes = 0;
+    bool aux_recorded = false;       // a graph holds its address
+    KeptBuffer *aux_kept = nullptr;  // earlier ones that graphs hold
     // numbers that a kernel hands to the host (pinned), and when they are there: the conjugate gradients' (made when first used)
     double *pin = nullptr;
     hipEvent_t pin_ready = nullptr;
