@@ -186,7 +186,7 @@ def _attn(q, k, v, scale, causal, q_len, k_len, bias):
             raise TypeError("bias must be a float32 GPU tensor of (sets, keys) with unit inner stride")
         at, ld = bias.data_ptr(), bias.stride(0) if batch > 1 else m
     return _ATTN.pack(*_heads(q, "q", q.shape, dtype), *_heads(k, "k", kv, dtype), *_heads(v, "v", kv, dtype), _DTYPES[dtype], 1 if causal else 0,
-                      batch, n, m, heads, kv_heads, d, d ** -0.5 if scale is None else scale, _lengths(q_len, "q_len", batch),
+                      batch, n, m, heads, kv_heads, d, max(d, 1) ** -0.5 if scale is None else scale, _lengths(q_len, "q_len", batch),
                       _lengths(k_len, "k_len", batch), at, ld)
 
 
