@@ -410,7 +410,9 @@ fs_status fs_points_release(fs_ctx *ctx);
  * |d_o_i| |v| / l_i, probabilities to 2^-40 of one, so keys that only rows of far smaller d_o see, or that no row gives a probability to
  * speak of, have gradients of fewer digits.
  * FS_BF16: products on the bf16 matrix cores with fp32 accumulation; probabilities (2^-9 of each) and their gradients are rounded to bf16
- * where they enter a second product.  Maxima, sums and accumulators are fp32 in both.
+ * where they enter a second product (in the backward pass of at most 32 rows a head of keys, to two bf16).
+ * Maxima, sums and accumulators are fp32 in both.  Probabilities are summed below a score that later ones may exceed by 2^30, so values
+ * beyond 2^97 / k_rows may overflow on the way.  A score that is NaN makes its row NaN, (m_i, l_i) too.
  */
 typedef struct {
     void *data;               /* element (set 0, row 0, head 0, coordinate 0); coordinates are contiguous */

@@ -202,8 +202,8 @@ __device__ inline void adam_block(void *const *at, int64_t i, int64_t n, uint32_
     }
 }
 
-// 1024 weights a workgroup, everything past the caches: an encoder of 31 million float weights 139 us (5.9 TB/s at 28 bytes a
-// weight; 165 with 4096 weights and through the caches), one of 101 million with bf16 weights, masters and 8-bit state 278 us (5.8 TB/s;
+// 1024 weights a workgroup, everything past the caches: an encoder of 31 million float weights 141 us a step (6.1 TB/s at 28 bytes a
+// weight; 165 with 4096 weights and through the caches), one of 101 million with bf16 weights, masters and 8-bit state 267 us (6.1 TB/s;
 // 320).  Small tensors: 4.5 us, a launch.
 template <typename P, typename G, bool MASTER, bool Q8> __global__ __launch_bounds__(256) void k_adamw(const Table<MASTER, Q8> tb, const AdamStep s)
 {

@@ -27,9 +27,10 @@ template <typename T> constexpr int min_waves(int dp) { return std::is_same<T, f
 // What a row reports as its largest score: NaN where a score is NaN, which fmaxf leaves out (of infinite scores the sum alone is NaN).
 __device__ inline float reported_max(float top, float sum) { return sum != sum && top < INFINITY ? sum : top; }
 
-// Bound by the vector ALU at d = 64 (two operations and an exp2 a score beside 2 d products: 16384 points, 16 heads, bf16: 1.22 ms, 900
-// TFLOP/s, vector ALU busy 75 %, matrix cores 46 %), by the matrix cores towards d = 128 (1000 TFLOP/s), by memory for one query (50021
-// keys, 4 sets, 8 heads of 128: 113 us, 5.9 TB/s).  S^T rather than S, since its registers are a row's probabilities in the order the next
+// Bound by the vector ALU at d = 64 (two operations and an exp2 a score beside 2 d products: 16384 points, 16 heads, bf16: 1.17 to 1.24 ms,
+// 890 to 940 TFLOP/s, vector ALU busy 76 %, matrix cores 47 %), by LDS and the matrix cores towards d = 128 (1060 TFLOP/s; 8192 points
+// under a causal line: 306 us, 900 TFLOP/s, busy 63 % and 42 %), by memory for one query (50021 keys, 4 sets, 8 heads of 128: 114 us,
+// 5.9 TB/s).  S^T rather than S, since its registers are a row's probabilities in the order the next
 // product takes them: they never pass through LDS.  32 rows a wave: two blocks of them a wave were slower (d = 64: 837 TFLOP/s and 843,
 // d = 128: 782 and 992), for their registers.
 // A workgroup has RW KS waves: wave w holds the w % RW-th 32 rows of the workgroup, and takes the w / RW-th part of every tile of KTS

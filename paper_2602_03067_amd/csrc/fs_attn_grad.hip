@@ -37,8 +37,9 @@ template <typename T> constexpr int dkv_waves(int dp)
 }
 
 // Rows in registers, keys streamed, as in k_attn: S^T = K Q^T and dP^T = V dO^T end as a row's ds in the order dQ^T += K^T dS^T takes them.
-// Three products a score; bound by the matrix cores and LDS together: 8192 points under a causal line, 16 heads of 128 over 4, bf16:
-// 430 us, 960 TFLOP/s; 64 heads of 1024 points, d = 64: 40 us, 650 TFLOP/s, one round of workgroups whose beginnings and ends show.
+// Three products a score; bound by LDS and the matrix cores together: 8192 points under a causal line, 16 heads of 128 over 4, bf16:
+// 438 us, 940 TFLOP/s, busy 59 % and 44 %; 64 heads of 1024 points, d = 64: 39 us, 650 TFLOP/s, one round of workgroups whose
+// beginnings and ends show.
 template <typename T, int DP, int KT, int WAVES, bool BIAS, Load LOAD, bool FINE>
 __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const AttnCall c)
 {
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(64 * WAVES, dq_waves<T>(DP)) void k_attn_dq(const A
 }
 
 // Keys in registers, rows streamed: S = Q K^T and dP = dO V^T end as a key's p and ds in the order dV^T += dO^T P and dK^T += Q^T dS take
-// them.  Four products a score; bound as k_attn_dq: 590 us, 930 TFLOP/s, and 51 us, 670 TFLOP/s, at the sizes there.  The products come one
+// them.  Four products a score; bound as k_attn_dq: 603 us, 910 TFLOP/s, and 50 us, 690 TFLOP/s, at the sizes there.  The products come one
 // after the other (d = 128 spills otherwise).
 template <typename T, int DP, int RT, int WAVES, bool BIAS, Load LOAD, bool FINE>
 __global__ __launch_bounds__(64 * WAVES, FINE && DP > 96 ? 1 : dkv_waves<T>(DP)) void k_attn_dkv(const AttnCall c)
@@ -669,9 +670,11 @@ template <typename T, int DP>
 fs_status run(Ctx *c, AttnCall a, const AttnGradPlan &p, char *ws, Load keys, Load rows_load)
 {
     using E = typename Mma<T>::Elem;
-    // A few rows for each head of keys: the roundings of p and ds do not average out, and the chip is idle.  Both go on as two bf16.  (One
-    // row, 153 keys, 16 heads over 4, d = 32: dk 1.7e-3 off 64 bits, which is its own rounding, and 2.8e-3 otherwise,
-    // 19 us both; 32 rows, 2000 keys, four sets, 8 heads of 128: 44 and 39 us.)
+    // p and ds as two bf16 where a head of keys has at most 32 rows: what is left of the error is the outputs' own rounding, 1.7e-3 of
+    // their norm; with one it is 2.4e-3, for any number of rows.  The line is drawn by what it costs.  Up to 32 rows, one tile, the pass
+    // is bound by its keys: one row, 153 keys, 16 heads over 4, d = 32 19 us both, 32 rows, 2000 keys, four sets, 8 heads of 128 39 us with
+    // one piece and 44 with two.  Beyond, the products bind: 64 rows there 42 and 51, 128 rows 52 and 62; 8 sets of 1024, 8 heads of 64,
+    // 81 and 106; 4096 points, 8 heads of 128, 270 and 390.
     constexpr bool kBf16 = std::is_same<T, __bf16>::value, kPairs = std::is_same<T, Pair>::value;
     const bool fine = kBf16 && (int64_t)a.n * a.group <= 32;
     Arena A;

@@ -66,7 +66,7 @@ template <int N> __device__ inline void load_row(const float *row, int col, int 
     }
 }
 
-// Bound by latency at the sizes that gain from pairs (three sets of 1000 and 777 points, 4 heads of 40, four tensors: 5.7 us, and 7.3 for
+// Bound by latency at the sizes that gain from pairs (three sets of 1000 and 777 points, 4 heads of 40, four tensors: 6.1 us, and 7.9 for
 // the second pass, of which some 2 are each launch's own).
 // Eight lanes take a row, each DP / 8 elements of it; a workgroup 32 rows at a time
 template <int DP> __global__ __launch_bounds__(256) void k_pair_max(const AttnCall c, bool aligned)

@@ -118,7 +118,7 @@ struct NormCall {
     bool past;                  // outputs that no cache will hold until they are read go past them
 };
 
-// 70000 x 784 float: 80 us, 5.5 TB/s; 50000 x 1024 bf16: 33 us, 6.2 TB/s.
+// 70000 x 784 float: 82 us, 5.4 TB/s; 50000 x 1024 bf16: 33 us, 6.2 TB/s.
 template <typename T, typename W, int VEC, int NV, int TPR, bool PAST>
 __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_norm(const NormCall c)
 {
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_nor
     if (t == 0 && c.stat) *(float2 *)(c.stat + 2 * row) = make_float2(mean + rest, rstd);
 }
 
-// 70000 x 784 float: 115 us, 5.7 TB/s; 50000 x 1024 bf16: 52 us, 5.9 TB/s; the workgroups' shares of the weights' gradients: k_norm_wsum, 5 us.
+// 70000 x 784 float: 117 us, 5.6 TB/s; 50000 x 1024 bf16: 52 us, 5.9 TB/s; the workgroups' shares of the weights' gradients: k_norm_wsum, 5 us.
 template <typename T, typename W, int VEC, int NV, int TPR, bool PAST>
 __global__ __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) void k_norm_grad(const NormCall c)
 {
