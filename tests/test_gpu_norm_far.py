@@ -32,3 +32,18 @@ def test_gradients_of_rows_far_from_zero(ctx, rows, cols, mean, dtype):
     close("dx", dx, want["dx"], TOL[dtype])
     close("dgamma", dg, want["dgamma"], 5e-6, want["terms"])
     close("dbeta", db, want["dbeta"], 5e-6, want["plain"])
+
+
+@pytest.mark.parametrize("cols", [300, 16384, 20001])
+def test_weights_alone_and_in_place_are_the_same(ctx, cols):
+    """The weights' gradients do not depend on whether dx is wanted, or takes dy's place."""
+    say("norm far, weights alone %d" % cols)
+    x, dy = normal(1, F32, 11, cols) + 1000.0, normal(2, F32, 11, cols)
+    _, stat = ctx.fs_layer_norm(x)
+    dx, dg, db = ctx.fs_layer_norm_grad(x, None, stat, dy)
+    for at in (None, dy.clone()):
+        given = dy if at is None else at
+        dw = torch.empty(2, cols, device="cuda")
+        assert ctx.lib.fs_layer_norm_grad(ctx.h, x.data_ptr(), 0, 11, cols, cols, None, 0, stat.data_ptr(), given.data_ptr(), cols,
+                                          None if at is None else at.data_ptr(), cols, dw.data_ptr(), dw.data_ptr() + 4 * cols) == 0
+        assert torch.equal(dw[0], dg) and torch.equal(dw[1], db) and (at is None or torch.equal(at, dx))
