@@ -397,7 +397,9 @@ fs_status fs_points_release(fs_ctx *ctx);
  * over the keys j that row i of a set sees: j < k_len, and with `causal` also j <= i + k_len - q_len (the last query sees the
  * last key).  Rows i >= q_len, and rows that see no key or only keys with bias -inf, have o_i = 0, m_i = -inf, l_i = 0
  * and pass no gradient on.  Keys that are not seen by any row (j >= k_len, or bias -inf) are not read into the result whatever
- * they hold, NaN included, and their gradients are 0.  A bias of the type's lowest value is a number like any other.
+ * they hold, NaN included, and their gradients are 0.  A key that only the rows from a causal line on see is one that is seen: NaN and
+ * infinities in its value (in the backward pass in the key too) may show in the rows of its block before the line as well, as zero
+ * times them.  A bias of the type's lowest value is a number like any other.
  * kv_heads divides q_heads; head h reads keys and values of head h / (q_heads / kv_heads).  d <= 128 coordinates.
  * Lengths may be 0 and 1, strides are in elements, any alignment will do (rows of whole 16 bytes, aligned to them, are
  * read fastest).
