@@ -1,6 +1,6 @@
 // Floats as pairs of fp16 for attention in full precision (see Pair in fs_attn.h): two passes over q, k, v and do, one for the largest
-// magnitude (and row norm) of every head, one that writes the pieces as the attention kernels' LDS tiles.  Any strides, lengths and
-// removed keys end here: what is not admitted becomes zero.
+// magnitude (and row norm) of every head, one that writes the pieces as the attention kernels' LDS tiles, and of do each row's scale, norm
+// and product with o, which the backward pass takes up.  Any strides, lengths and removed keys end here: what is not admitted becomes zero.
 #include <algorithm>
 
 #include "fs_attn.h"
